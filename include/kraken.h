@@ -64,7 +64,8 @@ typedef enum {
 typedef enum {
   KRAKEN_DTYPE_F32 = 0,
   KRAKEN_DTYPE_BF16 = 1,
-  KRAKEN_DTYPE_F16 = 2
+  KRAKEN_DTYPE_F16 = 2,
+  KRAKEN_DTYPE_E4M3 = 3        /* 8-bit floats (OCP e4m3, no infinities): paged caches only */
 } kraken_dtype;
 
 /* MFMA operand type of every projection and of attention (accumulation is
@@ -485,6 +486,149 @@ kraken_status kraken_op_decode_attention_noalloc(int32_t dtype, const void* qk,
                                                  const int32_t* lens, int32_t num_seqs,
                                                  int32_t max_seqs, int32_t capacity,
                                                  void* stream);
+
+/* ------------------------------------------------------------------------
+ * Paged KV cache.  A server that holds many conversations of unknown length keeps the keys
+ * and values of one layer in pages of page_size tokens that any sequence may own, instead of
+ * one slot of `capacity` tokens per sequence:
+ *   pages   device, 16-byte aligned:
+ *           [n_sub][2 (K, V)][num_pages][n_kv_heads][page_size][head_dim] elements of dtype
+ *   table   device int32, row b at table + b * table_ld: position p of sequence b lies in page
+ *           table[b][p / page_size], place p % page_size.  Sequences may share pages that
+ *           nothing appends to.  Entries that no position below needs are never read.
+ *   scales  dtype E4M3: device float32 [n_sub][2][n_kv_heads]; an element stands for
+ *           scale * its value.  NULL for the other types.
+ *   num_seqs       rows of the table, 1 .. KRAKEN_MAX_SEQS
+ *   pages_per_seq  entries of a row (a sequence's capacity is pages_per_seq * page_size, below
+ *                  2^31); table_ld >= pages_per_seq
+ *   head_dim       32, 64 or 128 (other head sizes are stored padded with zeros, as the model's)
+ * The table, positions and lengths are read on the device when the work runs, so a captured
+ * graph follows them from replay to replay.  The host cannot check them: an index that is out
+ * of range is never followed.  The row it belongs to is left out as stated at each call, and
+ * *fault (device int32, or NULL) is set to 1; calls never clear it.
+ */
+typedef struct {
+  void* pages;
+  const int32_t* table;
+  const float* scales;
+  int32_t dtype;
+  int32_t n_sub;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t num_pages;
+  int32_t page_size;
+  int32_t num_seqs;
+  int32_t pages_per_seq;
+  int32_t table_ld;
+} kraken_paged_cache;
+
+/* Rows of n_sub sub-layers: element c of row t of sub-layer i at
+ * data + i * sub_stride + t * row_stride + c (strides in elements, at least 0; data and the
+ * strides aligned to 16 bytes).  The columns Q | K | V of one projection are three of these. */
+typedef struct {
+  void* data;
+  int64_t sub_stride;
+  int64_t row_stride;
+} kraken_rows;
+
+/* Bytes of cache->pages; 0 for a NULL cache or one with sizes out of range (the pointers, the
+ * table and the scales are not looked at). */
+size_t kraken_paged_cache_bytes(const kraken_paged_cache* cache);
+
+/*
+ * kraken_op_paged_append: T new token rows into the cache, their queries and keys rotated by
+ * their positions on the way (kv_append of kraken_decode, for pages; KRAKEN_ARCH_* models have
+ * learned positions and append with rot_dim = 0).
+ *   q        rows of n_heads * head_dim elements of `dtype` (F32, BF16 or F16), or NULL
+ *   k, v     rows of n_kv_heads * head_dim elements of `dtype`
+ *   q_out    rotated queries (NULL if and only if q is; q_out = q, with the same strides,
+ *            rotates in place)
+ *   k_out    NULL, or rotated keys as rows (may be k, in place): with q_out what
+ *            kraken_op_attention reads of a prompt
+ *   pos      device int32 [T]: position of row t in its sequence, its place in the cache and
+ *            the factor of its angles.  Negative: a padding row, of which nothing is written.
+ *   seq      device int32 [T]: sequence (row of the table) of row t; NULL: row t is sequence t
+ *            (T <= num_seqs)
+ *   inv_freq HOST double [rot_dim / 2], finite: row t turns pair j by the angle
+ *            pos[t] * inv_freq[j] (radians, computed in 64 bits: no precision is lost at far
+ *            positions).  May be NULL if rot_dim is 0.
+ *   rot_dim  the first rot_dim dimensions of every head are rotated, a multiple of 8 in
+ *            0 .. head_dim (0: none)
+ *   neighbours  0: pair j is dimensions j and j + rot_dim / 2; otherwise 2 j and 2 j + 1.  A pair
+ *            (a, b) becomes (a cos - b sin, a sin + b cos), computed in fp32 and rounded once.
+ *   cache    dtype equal to `dtype`, or E4M3 with `dtype` BF16 or F16: elements are divided by
+ *            their scale, clamped to +-448 and rounded to the nearest even (a NaN stays one)
+ * Positions that no row names keep what they held.  Two rows of one call must not name one
+ * place.  Apart from in-place rotation the buffers must not overlap.
+ * A row whose seq, position or page is out of range writes nothing and sets *fault.
+ * T = 0 does nothing.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ */
+kraken_status kraken_op_paged_append(int32_t dtype, const kraken_rows* q, const kraken_rows* k,
+                                     const kraken_rows* v, const kraken_rows* q_out,
+                                     const kraken_rows* k_out, int32_t T, int32_t n_heads,
+                                     const int32_t* pos, const int32_t* seq,
+                                     const double* inv_freq, int32_t rot_dim, int32_t neighbours,
+                                     const kraken_paged_cache* cache, int32_t* fault,
+                                     void* stream);
+
+/*
+ * kraken_op_paged_attention: attention of one new token per sequence over its pages
+ * (kraken_op_decode_attention for a paged cache):
+ *   out[i][b] = softmax(scale * q K^T) V per head over positions 0 .. lens[b] - 1 of sequence b.
+ *   q        row b is sequence b's query, n_heads * head_dim elements of `dtype` (F32, BF16 or
+ *            F16); query head h reads key/value head h / (n_heads / n_kv_heads)
+ *   out      rows of n_heads * head_dim elements of `dtype`, not overlapping the inputs
+ *   lens     device int32 [num_seqs]: tokens that sequence b attends to, the new token's own,
+ *            which the append has written, among them.  0: a padding row, its output is zeros.
+ *   max_len  HOST: no lens[b] exceeds it, 0 .. pages_per_seq * page_size.  The launch is sized
+ *            by it: the tighter it is, the better.
+ *   scale    factor of the scores; 0 means 1 / sqrt(head_dim)
+ *   cache    dtype equal to `dtype`, or E4M3 with `dtype` BF16 or F16
+ *   work     device float32 scratch, 16-byte aligned, of work_floats >=
+ *            kraken_paged_attention_work_floats(cache, n_heads, max_len); NULL if that is 0.
+ *            It need not hold anything; calls that may run at one time need one each.
+ * Scores, softmax and sums are fp32.  Positions at or past lens[b] are never read.  The same
+ * call gives the same bits.  A row whose length is out of range (0 .. max_len) or that needs a
+ * page out of range gives NaN and sets *fault.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ * kraken_paged_attention_work_floats: the scratch such a call needs; -1 for sizes that the call
+ * refuses (the cache's pointers are not looked at).
+ */
+int64_t kraken_paged_attention_work_floats(const kraken_paged_cache* cache, int32_t n_heads,
+                                           int32_t max_len);
+kraken_status kraken_op_paged_attention(int32_t dtype, const kraken_rows* q,
+                                        const kraken_rows* out, int32_t n_heads,
+                                        const kraken_paged_cache* cache, const int32_t* lens,
+                                        int32_t max_len, float scale, float* work,
+                                        int64_t work_floats, int32_t* fault, void* stream);
+
+/*
+ * kraken_op_token_logprobs: what rows of logits (kraken_forward_tokens', or an unembedding by
+ * kraken_op_gemm) say about tokens.  With p = softmax(logits[r]) over `vocab` elements:
+ *   logits    `dtype` (F32, BF16 or F16), row r at logits + r * ld (ld >= vocab elements; any
+ *             alignment of an element)
+ *   tokens    device int32 [rows], or NULL
+ *   logprob   float32 [rows]: log p[tokens[r]]; 0 for a negative token (a padding row), NaN for
+ *             one at or past vocab.  NULL if and only if tokens is.
+ *   entropy   float32 [rows], or NULL: -sum p log p in nats (an element of -inf adds 0)
+ *   top       0 .. min(vocab, KRAKEN_MAX_TOP) most likely tokens of every row:
+ *   top_ids, top_logprobs   int32 and float32 [rows][top], the likeliest first, equal logits by
+ *             ascending index; NULL if and only if top is 0
+ *   work      device float32 scratch, 16-byte aligned, of work_floats >=
+ *             kraken_token_logprobs_work_floats(rows, vocab, top); NULL if that is 0.  As for
+ *             kraken_op_paged_attention.
+ * Computed in fp32.  A row that holds a NaN or +inf, or nothing but -inf, has no distribution:
+ * its log probabilities and entropy are NaN (its top_ids are still the largest logits, a NaN
+ * counting as larger than +inf).  rows = 0 does nothing.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ * kraken_token_logprobs_work_floats: the scratch such a call needs; -1 for sizes that the call
+ * refuses.
+ */
+#define KRAKEN_MAX_TOP 64
+int64_t kraken_token_logprobs_work_floats(int32_t rows, int32_t vocab, int32_t top);
+kraken_status kraken_op_token_logprobs(int32_t dtype, const void* logits, int64_t ld,
+                                       int32_t rows, int32_t vocab, const int32_t* tokens,
+                                       float* logprob, float* entropy, int32_t top,
+                                       int32_t* top_ids, float* top_logprobs, float* work,
+                                       int64_t work_floats, void* stream);
 
 #ifdef __cplusplus
 }

@@ -27,9 +27,12 @@ SOURCES = [
       for src in ("gemm_tile", "gemm_mid", "gemm_skinny") for t in ("f16", "bf16", "float")],
     ("attention.hip", "attention", []), ("gemm.hip", "gemm_dispatch", []),
     ("norm.hip", "norm", []), ("decode.hip", "decode", []), ("runtime.hip", "runtime", []),
+    ("paged_append.hip", "paged_append", []), ("paged_attention.hip", "paged_attention", []),
+    ("logprobs.hip", "logprobs", []),
 ]
 # one relocatable object per component (the GEMM's parts are merged into gemm.o)
-OBJECTS = ["gemm", "attention", "norm", "decode", "runtime"]
+OBJECTS = ["gemm", "attention", "norm", "decode", "runtime", "paged_append", "paged_attention",
+           "logprobs"]
 
 COMMON_FLAGS = [
     "-std=c++17", "-O3", "-fPIC", f"--offload-arch={ARCH}",

@@ -276,6 +276,9 @@ hipError_t launch_decode_attention(DType dt, const void* qk, const void* cache_l
                                    int d, int n_heads, int n_kv_heads, const int32_t* lens_host,
                                    int max_seqs, int capacity, int q_prescaled, hipStream_t s);
 
+// Keeps msg for kraken_last_error of this thread and returns status (a kraken_status).
+int set_error(int status, const char* msg) noexcept;
+
 // p[k] *= c for k < count (operand type dt).
 hipError_t launch_scale(DType dt, void* p, int64_t count, float c, hipStream_t s);
 

@@ -38,9 +38,21 @@
 
 using namespace kraken;
 
-namespace {
+namespace kraken {
 
 thread_local std::string g_last_error;
+
+int set_error(int status, const char* msg) noexcept {
+  try {
+    g_last_error = msg;
+  } catch (...) {                    // no memory for the text: the status stands alone
+  }
+  return status;
+}
+
+}  // namespace kraken
+
+namespace {
 
 // Scratch of the allocation-free decode attention (kraken_op_decode_attention_noalloc): the
 // per-chunk (max, sum, output) partials, fp32.  One copy per GPU, held until the process
@@ -52,8 +64,7 @@ float* g_scratch_ptr[kMaxDevices] = {};
 std::mutex g_scratch_mutex;
 
 kraken_status fail(kraken_status st, const std::string& msg) {
-  g_last_error = msg;
-  return st;
+  return (kraken_status)set_error((int)st, msg.c_str());
 }
 
 kraken_status hip_fail(hipError_t e, const char* what) {

@@ -11,7 +11,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import os
-from typing import Iterable, List, Mapping, Optional, Sequence, Tuple
+from typing import Iterable, List, Mapping, NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
@@ -19,11 +19,12 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libkraken.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_OOM, ERR_STATE, ERR_HIP, ERR_OVERFLOW = range(7)
-DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
+DTYPE_F32, DTYPE_BF16, DTYPE_F16, DTYPE_E4M3 = 0, 1, 2, 3
 COMPUTE_CODES = {"storage": 0, "f32": 1, "bf16": 2, "f16": 3}
 MAX_SEQS = 256
 # floats of the static scratch of kraken_op_decode_attention_noalloc (kraken.h)
 NOALLOC_SCRATCH_FLOATS = 8 * 1024 * 1024
+MAX_TOP = 64                     # most likely tokens kraken_op_token_logprobs can name
 
 ARCH_CODES = {"kraken": 0, "gpt": 1, "parallel": 2}
 
@@ -57,6 +58,20 @@ class _Config(ctypes.Structure):
                 ("ln_eps", ctypes.c_float), ("n_kv_heads", ctypes.c_int32),
                 ("arch", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("vocab", ctypes.c_int32), ("max_positions", ctypes.c_int32)]
+
+
+class _PagedCache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("scales", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("n_sub", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("num_seqs", ctypes.c_int32),
+                ("pages_per_seq", ctypes.c_int32), ("table_ld", ctypes.c_int32)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("sub_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -102,6 +117,15 @@ def lib() -> ctypes.CDLL:
                                         i32, vp, i64, vp], i32),
         "kraken_op_decode_attention_noalloc": ([i32, vp, vp, vp, i32, i32, i32, i32, P(i32),
                                                 i32, i32, i32, vp], i32),
+        "kraken_paged_cache_bytes": ([P(_PagedCache)], sz),
+        "kraken_op_paged_append": ([i32, P(_Rows), P(_Rows), P(_Rows), P(_Rows), P(_Rows), i32,
+                                    i32, vp, vp, vp, i32, i32, P(_PagedCache), vp, vp], i32),
+        "kraken_paged_attention_work_floats": ([P(_PagedCache), i32, i32], i64),
+        "kraken_op_paged_attention": ([i32, P(_Rows), P(_Rows), i32, P(_PagedCache), vp, i32, fp,
+                                       vp, i64, vp, vp], i32),
+        "kraken_token_logprobs_work_floats": ([i32, i32, i32], i64),
+        "kraken_op_token_logprobs": ([i32, vp, i64, i32, i32, vp, vp, vp, i32, vp, vp, vp, i64,
+                                      vp], i32),
     }
     for name, (args, res) in sigs.items():
         fn = getattr(L, name)
@@ -525,3 +549,253 @@ def op_decode_attention_noalloc(qk: torch.Tensor, kv_layer: torch.Tensor, out: t
                                                     kv_layer.data_ptr(), out.data_ptr(), n, d,
                                                     n_heads, n_kv_heads, arr, B, max_seqs,
                                                     capacity, _stream(stream)))
+
+
+# ----------------------------------------------------------------- paged cache and log probabilities
+
+_ROW_CODES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
+_CACHE_CODES = {**_ROW_CODES, torch.float8_e4m3fn: DTYPE_E4M3}
+
+
+def _check_gpu(name: str, t: torch.Tensor, device: Optional[torch.device]) -> None:
+    if not getattr(t, "is_cuda", False):
+        raise ValueError(f"{name} must be a GPU tensor (got {getattr(t, 'device', type(t))})")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+
+
+def _check_current(device: torch.device) -> None:
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {device}, which is not the current device")
+
+
+def _rows(name: str, t: torch.Tensor, dtype: torch.dtype, shape, device) -> _Rows:
+    """Rows [n][T][width] for the C ABI: elements of a row are adjacent, any other strides."""
+    _check_gpu(name, t, device)
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must have dtype {dtype} (got {t.dtype})")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    sub, row, col = t.stride()
+    if col != 1:
+        raise ValueError(f"the elements of {name}'s rows must be adjacent")
+    return _Rows(t.data_ptr(), sub, row)
+
+
+def _ints(name: str, t: Optional[torch.Tensor], shape, device) -> Optional[int]:
+    """Address of a contiguous int32 GPU tensor (None: NULL)."""
+    if t is None:
+        return None
+    _check_gpu(name, t, device)
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} "
+                         f"(got {t.dtype} {tuple(t.shape)})")
+    return t.data_ptr()
+
+
+def _floats(name: str, t: Optional[torch.Tensor], shape, device) -> Optional[int]:
+    """Address of a contiguous float32 GPU tensor (None: NULL)."""
+    if t is None:
+        return None
+    _check_gpu(name, t, device)
+    if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 tensor of shape {shape} "
+                         f"(got {t.dtype} {tuple(t.shape)})")
+    return t.data_ptr()
+
+
+def _paged(pages: torch.Tensor, table: torch.Tensor, scales: Optional[torch.Tensor],
+           device=None) -> _PagedCache:
+    """The description of a paged cache: pages [n][2 (K, V)][num_pages][kv_heads][page_size]
+    [head_dim], contiguous; table [num_seqs][pages_per_seq] int32, rows of adjacent entries."""
+    _check_gpu("pages", pages, device)
+    device = pages.device
+    code = _CACHE_CODES.get(pages.dtype)
+    if code is None:
+        raise ValueError(f"pages cannot have dtype {pages.dtype}")
+    if pages.dim() != 6 or pages.shape[1] != 2 or not pages.is_contiguous():
+        raise ValueError("pages must be a contiguous tensor "
+                         "[n][2][num_pages][kv_heads][page_size][head_dim]")
+    _check_gpu("table", table, device)
+    if table.dtype != torch.int32 or table.dim() != 2 or table.stride(1) != 1:
+        raise ValueError("table must be int32 [num_seqs][pages_per_seq] with adjacent entries")
+    n, _, num_pages, heads, page_size, hd = pages.shape
+    seqs, per_seq = table.shape
+    ld = table.stride(0) if seqs > 1 else per_seq
+    return _PagedCache(pages.data_ptr(), table.data_ptr(),
+                       _floats("scales", scales, (n, 2, heads), device), code, n, heads, hd,
+                       num_pages, page_size, seqs, per_seq, ld)
+
+
+def _new(shape, dtype: torch.dtype, device, stream) -> torch.Tensor:
+    """An uninitialised tensor of the allocator's pool of `stream` (None: the current one), so
+    that its memory is free for work on that stream, and returns to it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _work(need: int, work: Optional[torch.Tensor], device, stream):
+    """(keep-alive, address, floats) of a workspace: the caller's, or a new one."""
+    if need < 0:
+        return None, None, 0        # sizes that the call itself refuses
+    if work is None:
+        if need == 0:
+            return None, None, 0
+        work = _new((need,), torch.float32, device, stream)
+    _check_gpu("work", work, device)
+    if work.dtype != torch.float32 or not work.is_contiguous():
+        raise ValueError("work must be a contiguous float32 tensor")
+    return work, work.data_ptr(), work.numel()
+
+
+def new_paged_cache(n: int, n_kv_heads: int, head_dim: int, num_pages: int, page_size: int,
+                    dtype, device=None) -> torch.Tensor:
+    """Pages (uninitialised) of one layer's paged cache, [n][2 (K, V)][num_pages][n_kv_heads]
+    [page_size][head_dim]; dtype "f32", "bf16", "f16", "e4m3" or a torch dtype."""
+    dt = torch.float8_e4m3fn if dtype in ("e4m3", torch.float8_e4m3fn) \
+        else torch_dtype(dtype_code(dtype))
+    c = _PagedCache(None, None, None, _CACHE_CODES[dt], n, n_kv_heads, head_dim, num_pages,
+                    page_size, 1, 1, 1)
+    if lib().kraken_paged_cache_bytes(ctypes.byref(c)) == 0:
+        raise ValueError("sizes that no paged cache has")
+    return torch.empty((n, 2, num_pages, n_kv_heads, page_size, head_dim), dtype=dt,
+                       device=device or "cuda")
+
+
+def op_paged_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+                    pages: torch.Tensor, table: torch.Tensor, pos: torch.Tensor,
+                    q_out: Optional[torch.Tensor] = None, seq: Optional[torch.Tensor] = None,
+                    k_out: Optional[torch.Tensor] = None,
+                    inv_freq: Optional[torch.Tensor] = None, neighbours: bool = False,
+                    scales: Optional[torch.Tensor] = None, fault: Optional[torch.Tensor] = None,
+                    stream=None) -> Optional[torch.Tensor]:
+    """New token rows into a paged cache, queries and keys rotated by their positions
+    (kraken_op_paged_append).  q [n, T, heads * hd] or None, k and v [n, T, kv_heads * hd];
+    pos (and seq) int32 [T] on the GPU, a negative position is a padding row; inv_freq: radians
+    per position of the rotated pairs, a float64 tensor on the host (None: no rotation).
+    Returns q_out (new if not given; q itself rotates in place)."""
+    cache = _paged(pages, table, scales)
+    device, hd = pages.device, cache.head_dim
+    if k.dim() != 3:
+        raise ValueError("k must be [n][T][kv_heads * head_dim]")
+    n, T, dkv = cache.n_sub, k.shape[1], cache.n_kv_heads * hd
+    code = _ROW_CODES.get(k.dtype)
+    if code is None:
+        raise ValueError(f"k cannot have dtype {k.dtype}")
+    rk = _rows("k", k, k.dtype, (n, T, dkv), device)
+    rv = _rows("v", v, k.dtype, (n, T, dkv), device)
+    rq = ro = None
+    heads = cache.n_kv_heads
+    if q is not None:
+        if q.dim() != 3 or q.shape[2] % hd:
+            raise ValueError("q must be [n][T][heads * head_dim]")
+        heads = q.shape[2] // hd
+        rq = _rows("q", q, k.dtype, (n, T, heads * hd), device)
+        if q_out is None:
+            q_out = _new((n, T, heads * hd), k.dtype, device, stream)
+        ro = _rows("q_out", q_out, k.dtype, (n, T, heads * hd), device)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    rko = None if k_out is None else _rows("k_out", k_out, k.dtype, (n, T, dkv), device)
+    freq, rot = None, 0
+    if inv_freq is not None:
+        if inv_freq.is_cuda or inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 \
+                or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be a contiguous float64 vector on the host")
+        freq, rot = inv_freq.data_ptr(), 2 * inv_freq.numel()
+    fault_at = _ints("fault", fault, (1,), device)
+    pos_at, seq_at = _ints("pos", pos, (T,), device), _ints("seq", seq, (T,), device)
+    _check_current(device)
+    if T == 0:
+        return q_out
+    _check(lib().kraken_op_paged_append(code, rq, rk, rv, ro, rko, T, heads, pos_at, seq_at,
+                                        freq, rot, 1 if neighbours else 0, cache, fault_at,
+                                        _stream(stream)))
+    return q_out
+
+
+def op_paged_attention(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor,
+                       lens: torch.Tensor, max_len: int, out: Optional[torch.Tensor] = None,
+                       scale: float = 0.0, scales: Optional[torch.Tensor] = None,
+                       work: Optional[torch.Tensor] = None,
+                       fault: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of one new token per sequence over its pages (kraken_op_paged_attention).
+    q [n, num_seqs, heads * hd]; lens int32 [num_seqs] on the GPU, none above max_len.  work: a
+    float32 workspace of paged_attention_work_floats elements (None: a new one)."""
+    cache = _paged(pages, table, scales)
+    device, hd = pages.device, cache.head_dim
+    if q.dim() != 3 or q.shape[2] % hd:
+        raise ValueError("q must be [n][num_seqs][heads * head_dim]")
+    code = _ROW_CODES.get(q.dtype)
+    if code is None:
+        raise ValueError(f"q cannot have dtype {q.dtype}")
+    shape = (cache.n_sub, cache.num_seqs, q.shape[2])
+    rq = _rows("q", q, q.dtype, shape, device)
+    lens_at = _ints("lens", lens, (cache.num_seqs,), device)
+    if lens_at is None:
+        raise ValueError("lens is None")
+    fault_at = _ints("fault", fault, (1,), device)
+    heads = q.shape[2] // hd
+    if out is None:
+        out = _new(shape, q.dtype, device, stream)
+    ro = _rows("out", out, q.dtype, shape, device)
+    need = lib().kraken_paged_attention_work_floats(cache, heads, max_len)
+    work, work_at, floats = _work(need, work, device, stream)
+    _check_current(device)
+    _check(lib().kraken_op_paged_attention(code, rq, ro, heads, cache, lens_at, max_len, scale,
+                                           work_at, floats, fault_at, _stream(stream)))
+    return out
+
+
+def paged_attention_work_floats(pages: torch.Tensor, table: torch.Tensor, n_heads: int,
+                                max_len: int) -> int:
+    """float32 elements of the workspace of op_paged_attention for a cache."""
+    n, _, num_pages, heads, page_size, hd = pages.shape
+    c = _PagedCache(None, None, None, _CACHE_CODES[pages.dtype], n, heads, hd, num_pages,
+                    page_size, table.shape[0], table.shape[1], table.shape[1])
+    return int(lib().kraken_paged_attention_work_floats(c, n_heads, max_len))
+
+
+class TokenLogprobs(NamedTuple):
+    logprob: Optional[torch.Tensor]          # [rows], of the given tokens
+    entropy: torch.Tensor                    # [rows], nats
+    top_ids: Optional[torch.Tensor]          # [rows, top], the likeliest first
+    top_logprobs: Optional[torch.Tensor]     # [rows, top]
+
+
+def op_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0,
+                      work: Optional[torch.Tensor] = None, stream=None) -> TokenLogprobs:
+    """Log probabilities of tokens (int32 [rows]), the entropy and the `top` most likely tokens
+    of rows of logits [rows, vocab] (kraken_op_token_logprobs); rows of adjacent elements with
+    any stride between them."""
+    _check_gpu("logits", logits, None)
+    device = logits.device
+    code = _ROW_CODES.get(logits.dtype)
+    if code is None:
+        raise ValueError(f"logits cannot have dtype {logits.dtype}")
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be [rows][vocab] with adjacent elements")
+    rows, vocab = logits.shape
+    tokens_at = _ints("tokens", tokens, (rows,), device)
+    if not 0 <= top <= min(vocab, MAX_TOP):
+        raise ValueError(f"top must be in 0..min(vocab, {MAX_TOP})")
+    logprob = None if tokens is None else _new((rows,), torch.float32, device, stream)
+    entropy = _new((rows,), torch.float32, device, stream)
+    ids = _new((rows, top), torch.int32, device, stream) if top else None
+    best = _new((rows, top), torch.float32, device, stream) if top else None
+    need = lib().kraken_token_logprobs_work_floats(rows, vocab, top)
+    work, work_at, floats = _work(need, work, device, stream)
+    _check_current(device)
+    if rows:
+        _check(lib().kraken_op_token_logprobs(
+            code, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab,
+            tokens_at, _ptr(logprob), entropy.data_ptr(), top, _ptr(ids), _ptr(best), work_at,
+            floats, _stream(stream)))
+    return TokenLogprobs(logprob, entropy, ids, best)
+
+
+def token_logprobs_work_floats(rows: int, vocab: int, top: int = 0) -> int:
+    """float32 elements of the workspace of op_token_logprobs."""
+    return int(lib().kraken_token_logprobs_work_floats(rows, vocab, top))

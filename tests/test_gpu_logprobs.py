@@ -1,0 +1,151 @@
+"""Token log probabilities on the GPU, against log_softmax in 64 bits.
+
+Bound of a log probability (x - m) - log s: x - m rounds once (2^-24 |x - m|) and so does the
+difference; s, a sum of positive terms, is off by 2^-24 for each of the at most vocab / 64 + 64
+additions a term passes, and by the exponentials' own 2^-22 and their arguments' (weighted by the
+terms, at most 2^-23 (1 + entropy + log vocab)): (vocab / 64 + 64 + 48) 2^-24 in all, plus
+2^-22 |log s|.  The entropy log s - u / s adds the same for u, times 1 + |u / s|."""
+
+import math
+
+import pytest
+import torch
+
+from paper_2408_07802_amd import kraken as K
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def reference(x, tokens):
+    logp = torch.log_softmax(x.double(), 1)
+    p = logp.exp()
+    ent = -torch.where(p > 0, p * logp, 0.0).sum(1)
+    return logp, logp.gather(1, tokens.long()[:, None])[:, 0], ent
+
+
+def check(x, tokens, top, r, rows=None):
+    """Everything op_token_logprobs says of rows (default: all) of x."""
+    rows = torch.arange(x.shape[0], device=DEV) if rows is None else rows
+    x, tokens = x[rows], tokens[rows]
+    V = x.shape[1]
+    logp, lp, ent = reference(x, tokens)
+    base = (V / 64 + 64 + 48) * 2.0 ** -24 + 2.0 ** -22 * math.log(V + 1)
+    bound = base + 2.0 ** -22 * lp.abs()
+    assert bool(((r.logprob[rows].double() - lp).abs() <= bound).all())
+    assert bool(((r.entropy[rows].double() - ent).abs() <= base * (2 + 2 * ent)).all())
+    if top:
+        _, ids = torch.sort(x.float() + 0.0, dim=1, descending=True, stable=True)
+        ids = ids[:, :top]
+        assert torch.equal(r.top_ids[rows], ids.to(torch.int32))
+        best = logp.gather(1, ids)
+        got = r.top_logprobs[rows].double()
+        inf = best == -math.inf
+        assert torch.equal(got == -math.inf, inf)
+        assert bool(((got - best).abs() <= base + 2.0 ** -22 * best.abs())[~inf].all())
+
+
+def make(rows, vocab, dtype, seed, pad=0, offset=0):
+    g = torch.Generator(device="cpu").manual_seed(seed)
+    x = torch.randn((rows, vocab + pad), generator=g) * 3 + 10 * torch.randn((rows, 1),
+                                                                             generator=g)
+    flat = torch.empty(rows * (vocab + pad) + offset, dtype=dtype, device=DEV)
+    x = flat[offset:].view(rows, vocab + pad).copy_(x)[:, :vocab]
+    tokens = torch.randint(vocab, (rows,), generator=g).to(torch.int32).to(DEV)
+    return x, tokens
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16],
+                         ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,vocab,top,pad,offset", [
+    (1, 1, 1, 0, 0), (3, 2, 2, 0, 1), (5, 63, 63, 0, 0), (4, 64, 64, 1, 0), (2, 65, 5, 0, 3),
+    (7, 1000, 20, 3, 1), (1, 4099, 64, 0, 0), (300, 513, 1, 0, 0), (2, 50257, 20, 0, 0),
+    (1, 51200, 5, 0, 0), (3, 51200, 0, 0, 1), (1, 200003, 40, 0, 0), (61, 50257, 20, 47, 0),
+    (600, 2050, 64, 0, 0),
+])
+def test_rows(dtype, rows, vocab, top, pad, offset):
+    print(f"[logprobs] {rows} x {vocab} top {top} pad {pad} offset {offset} {dtype}", flush=True)
+    x, tokens = make(rows, vocab, dtype, rows + vocab, pad, offset)
+    r = K.op_token_logprobs(x, tokens, top=top)
+    check(x, tokens, top, r)
+    again = K.op_token_logprobs(x, tokens, top=top)
+    assert all(a is b or torch.equal(a, b) for a, b in zip(r, again))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16], ids=["f32", "f16"])
+@pytest.mark.parametrize("vocab", [70, 3000, 70001])
+def test_orders_and_ties(dtype, vocab):
+    """Rows whose order is the worst for a running list of the largest, and rows of ties."""
+    c = torch.arange(vocab, device=DEV, dtype=torch.float32)
+    rows = torch.stack([
+        c * (8.0 / vocab), -c * (8.0 / vocab), torch.zeros_like(c), c % 7, -(c % 5),
+        torch.where(c == vocab - 1, 1.0, 0.0), torch.where(c % 2 == 0, 0.0, -0.0),
+        torch.full_like(c, torch.finfo(dtype).min),
+        torch.where(c < 66, torch.finfo(dtype).min, -math.inf),
+        torch.where(c % 1000 == 69, 2.0, -math.inf)]).to(dtype)
+    tokens = torch.full((rows.shape[0],), 69, dtype=torch.int32, device=DEV)
+    tokens[8] = 65
+    for top in (1, 5, 64):
+        check(rows, tokens, top, K.op_token_logprobs(rows, tokens, top=top))
+
+
+def test_rows_without_a_distribution_and_padding():
+    V = 3001
+    x, tokens = make(8, V, torch.float32, 1)
+    x[1] = -math.inf
+    x[2, 5] = math.nan
+    x[3, 7] = math.inf
+    x[4, :] = math.nan
+    tokens[5], tokens[6] = -1, V
+    r = K.op_token_logprobs(x, tokens, top=3)
+    assert bool(r.logprob[1:5].isnan().all()) and bool(r.entropy[1:5].isnan().all())
+    assert bool(r.top_logprobs[1:5].isnan().all())
+    assert r.top_ids[1].tolist() == [0, 1, 2] and r.top_ids[4].tolist() == [0, 1, 2]
+    assert int(r.top_ids[2, 0]) == 5 and int(r.top_ids[3, 0]) == 7
+    assert float(r.logprob[5]) == 0.0 and math.isnan(float(r.logprob[6]))
+    check(x, tokens.clamp(0, V - 1), 3, r._replace(logprob=K.op_token_logprobs(
+        x, tokens.clamp(0, V - 1)).logprob), rows=torch.tensor([0, 5, 6, 7], device=DEV))
+    assert K.op_token_logprobs(x).logprob is None
+    e = K.op_token_logprobs(x[:0], tokens[:0], top=2)
+    assert e.logprob.shape == (0,) and e.top_ids.shape == (0, 2)
+
+
+def test_workspace_graph_and_streams():
+    x, tokens = make(4, 60000, torch.bfloat16, 3)
+    want = K.op_token_logprobs(x, tokens, top=8)
+    work = torch.full((max(4, K.token_logprobs_work_floats(4, 60000, 8)),), math.nan, device=DEV)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        got = K.op_token_logprobs(x, tokens, top=8, work=work)
+    for seed in (3, 4, 5):
+        y, t = make(4, 60000, torch.bfloat16, seed)
+        x.copy_(y)
+        tokens.copy_(t)
+        want = K.op_token_logprobs(x, tokens, top=8)
+        work.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    both = [K.op_token_logprobs(x, tokens, top=8, stream=s) for s in streams]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for r in both for a, b in zip(r, want))
+
+
+def test_scores_of_a_model_answer():
+    """What kraken_forward_tokens answers, scored: the greedy token is the likeliest, and the
+    log probabilities are those of its logits."""
+    cfg = K.Config(n_sub=2, n_layers=1, d_model=128, n_heads=2, d_ff=256, max_tokens=32,
+                   dtype="f16", vocab=1003, max_positions=32)
+    g = torch.Generator(device=DEV).manual_seed(0)
+    model = K.Kraken(cfg)
+    model.load_weights((torch.randn(K.weight_blob_elems(cfg), generator=g, device=DEV) * 0.05)
+                       .to(torch.float16))
+    logits, _ = model.forward_tokens(list(range(20)), [0, 7, 20])
+    greedy = logits.argmax(1).to(torch.int32)
+    r = K.op_token_logprobs(logits, greedy, top=5)
+    torch.cuda.synchronize()
+    model.close()
+    assert torch.equal(r.top_ids[:, 0], greedy) and torch.equal(r.top_logprobs[:, 0], r.logprob)
+    check(logits, greedy, 5, r)
