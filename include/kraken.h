@@ -501,6 +501,8 @@ kraken_status kraken_op_decode_attention_noalloc(int32_t dtype, const void* qk,
  *   num_seqs       rows of the table, 1 .. KRAKEN_MAX_SEQS
  *   pages_per_seq  entries of a row (a sequence's capacity is pages_per_seq * page_size, below
  *                  2^31); table_ld >= pages_per_seq
+ *   page_size      n_kv_heads * page_size * head_dim elements (one page of one sub-layer's keys)
+ *                  stay below 2^31 bytes
  *   head_dim       32, 64 or 128 (other head sizes are stored padded with zeros, as the model's)
  * The table, positions and lengths are read on the device when the work runs, so a captured
  * graph follows them from replay to replay.  The host cannot check them: an index that is out
@@ -580,7 +582,8 @@ kraken_status kraken_op_paged_append(int32_t dtype, const kraken_rows* q, const 
  *   out      rows of n_heads * head_dim elements of `dtype`, not overlapping the inputs
  *   lens     device int32 [num_seqs]: tokens that sequence b attends to, the new token's own,
  *            which the append has written, among them.  0: a padding row, its output is zeros.
- *   max_len  HOST: no lens[b] exceeds it, 0 .. pages_per_seq * page_size.  The launch is sized
+ *   max_len  HOST: no lens[b] exceeds it, 0 .. pages_per_seq * page_size, with num_seqs *
+ *            max_len below 2^35.  The launch is sized
  *            by it: the tighter it is, the better.
  *   scale    factor of the scores; 0 means 1 / sqrt(head_dim)
  *   cache    dtype equal to `dtype`, or E4M3 with `dtype` BF16 or F16

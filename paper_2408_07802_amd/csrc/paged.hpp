@@ -53,6 +53,13 @@ KRAKEN_HD int64_t paged_row(const PagedView& c, int i, int kv, int page, int h) 
   return ((((int64_t)i * 2 + kv) * c.pages + page) * c.heads + h) * (int64_t)c.page.d;
 }
 
+// A list of `total` items in `runs` (1 .. total) equal runs: the first item of run w, and the
+// last run that holds an item at or before `item` of its own.
+KRAKEN_HD int64_t split_begin(int64_t total, int runs, int w) { return total * w / runs; }
+KRAKEN_HD int split_last(int64_t total, int runs, int64_t item) {
+  return (int)(((item + 1) * runs - 1) / total);
+}
+
 // Checks a cache's description (with_data: its pointers, too) and fills view; a message and
 // *status otherwise.
 const char* paged_view(const kraken_paged_cache* cache, bool with_data, PagedView* view,

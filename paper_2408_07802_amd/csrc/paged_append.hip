@@ -168,6 +168,11 @@ const char* paged_view(const kraken_paged_cache* c, bool with_data, PagedView* v
   if (c->table_ld < c->pages_per_seq) return "table_ld is below pages_per_seq";
   if ((int64_t)c->pages_per_seq * c->page_size >= (1ll << 31))
     return "pages_per_seq * page_size must stay below 2^31";
+  const int es = c->dtype == KRAKEN_DTYPE_E4M3 ? 1 : c->dtype == KRAKEN_DTYPE_F32 ? 4 : 2;
+  if ((int64_t)c->n_kv_heads * c->head_dim * es * c->page_size >= (1ll << 31)) {
+    *status = KRAKEN_ERR_UNSUPPORTED;
+    return "a page of one sub-layer's keys must stay below 2^31 bytes";
+  }
   // (elements of the cache must fit 62 bits; the first three factors stay below 2^64)
   const double elems = 2.0 * c->n_sub * c->num_pages * c->n_kv_heads * (double)c->page_size *
                        c->head_dim;

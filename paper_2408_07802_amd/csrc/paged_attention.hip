@@ -1,6 +1,28 @@
 // Attention of one new token per sequence over a paged KV cache.
+//
+// Work: a unit is one (sub-layer, key/value head, block of up to 16 of its query heads) of one
+// sequence; its keys are cut into tiles of KT.  All tiles of all units stand in one list
+// (sequence by sequence), which W waves share in equal runs, whatever the sequences' lengths are:
+// the lengths are read on the device, so a replayed graph follows them.  A wave takes its run
+// tile by tile with a running maximum and sum per query head (online softmax, base 2), writes
+// the output of every unit that lies inside its run, and a partial (maximum, sum, output) of the
+// unit that its run begins or ends in the middle of; the join kernel merges those.  Waves share
+// nothing: there is no barrier.
+//
+// Tile: S^T = K Q^T and O^T += V^T P^T by 16 x 16 matrix instructions, keys x query heads and
+// features x query heads, so a lane keeps one query head (lane % 16) throughout and the maximum,
+// the sum and the rescaling are its own; the scores are the second product's operand as they
+// lie in registers.  Only few of the 16 columns are used where few query heads share a
+// key/value head; the products are cheap next to the tile's bytes all the same.
+//
+// Data: a tile's K and V rows (8 KB each) go from the pages straight into LDS, two tiles in
+// flight, and the page numbers of a tile's rows do so two tiles before that.  Chunks of 16 bytes
+// of a row are permuted so that the reads spread over all LDS banks; V is read transposed
+// (ds_read_b64_tr).
 #include <hip/hip_runtime.h>
 #include <math.h>
+
+#include <algorithm>
 
 #include "kraken_internal.hpp"
 #include "paged.hpp"
@@ -18,98 +40,615 @@ struct PagedAttnParams {
   PagedView cache;
   const int32_t* lens;
   int32_t* fault;
-  int heads, group, max_len;
+  int4* desc;           // [W]: units that begin in a run and do not end there (parts, b, u, 0)
+  float* ml;            // [W][2][qh][2]: maximum and sum
+  float* o;             // [W][2][qh][HD]: unnormalised output
+  int heads, group, max_len, W;
+  int qblocks, qh;      // blocks of query heads per key/value head; query heads per block (<= 16)
   float scale;
 };
 
 typedef uint8_t e4m3;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) void* lds_ptr;
 
-template <typename C>
-__device__ __forceinline__ void load8(const C* p, float* x) {
-  if constexpr (sizeof(C) == 1) {
-    const uint2 c = *reinterpret_cast<const uint2*>(p);
-    x[0] = __builtin_amdgcn_cvt_f32_fp8(c.x, 0);
-    x[1] = __builtin_amdgcn_cvt_f32_fp8(c.x, 1);
-    x[2] = __builtin_amdgcn_cvt_f32_fp8(c.x, 2);
-    x[3] = __builtin_amdgcn_cvt_f32_fp8(c.x, 3);
-    x[4] = __builtin_amdgcn_cvt_f32_fp8(c.y, 0);
-    x[5] = __builtin_amdgcn_cvt_f32_fp8(c.y, 1);
-    x[6] = __builtin_amdgcn_cvt_f32_fp8(c.y, 2);
-    x[7] = __builtin_amdgcn_cvt_f32_fp8(c.y, 3);
-  } else {
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return (uint32_t)(uintptr_t)(lds_ptr)p;
+}
+
+// 16 (4) bytes per lane from global memory into LDS at `lds` + 16 (4) * lane.  Counted by
+// vmcnt, which the kernel waits for itself.
+__device__ __forceinline__ void dma16(uint32_t lds, const void* g) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(g) : "memory", "m0");
+}
+__device__ __forceinline__ void dma4(uint32_t lds, const void* g) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+               :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(g) : "memory", "m0");
+}
+// Waits until at most N of the wave's vector memory operations are outstanding (they complete
+// in order).
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  static_assert(N < 64, "vmcnt has 6 bits");
+  asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory");
+}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Sizes of a tile.  C: the cache's element type.
+template <typename C, int HD>
+struct Tile {
+  static constexpr int RB = HD * (int)sizeof(C);               // bytes of a row
+  static constexpr int NC = RB / 16;                           // 16-byte chunks of a row
+  static constexpr int KT = 8192 / RB < 128 ? 8192 / RB : 128; // keys
+  static constexpr int RPI = 64 / NC;                          // rows per DMA instruction
+  static constexpr int NI = KT / RPI;                          // DMA instructions for K (for V)
+  static constexpr int NT = (KT + 63) / 64;                    // and for the page numbers
+  static constexpr int LINE = NC < 16 ? 16 / NC : 1;           // rows per 256 bytes of LDS
+};
+
+// Logical chunk c of row r lies at chunk c ^ key of its row.  K is read by 16 lanes that take
+// the same chunk of 16 consecutive rows: those fall on 16 different chunks of a 256-byte line.
+template <typename C, int HD>
+__device__ __forceinline__ int k_key(int r) {
+  using T = Tile<C, HD>;
+  return (r / T::LINE) & (T::NC < 16 ? T::NC - 1 : 15);
+}
+// V by 32 lanes at a time.  16 bits: two chunks of 8 consecutive rows (the pair stays together);
+// 8 bits: one chunk of rows r .. r + 7 and r + 16 .. r + 23; fp32: 16 chunks of one row.
+template <typename C, int HD>
+__device__ __forceinline__ int v_key(int r) {
+  using T = Tile<C, HD>;
+  if constexpr (sizeof(C) == 2) return ((r / T::LINE) & (T::NC / 2 - 1)) * 2;
+  if constexpr (sizeof(C) == 1)
+    return ((r / T::LINE) & (8 / T::LINE - 1)) | ((r >> 4) & 1) * (8 / T::LINE);
+  return 0;
+}
+
+template <typename S>
+using Vec8 = typename std::conditional<__is_same(S, bf16), bf16x8, f16x8>::type;
+
+template <typename S>
+__device__ __forceinline__ f32x4 mfma32(Vec8<S> a, Vec8<S> b, f32x4 c) {
+  if constexpr (__is_same(S, bf16))
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Eight e4m3 values as S (exact: S has more bits and a wider range).
+template <typename S>
+__device__ __forceinline__ Vec8<S> from_e4m3(uint32_t lo, uint32_t hi) {
+  Vec8<S> r;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)p[e];
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t w = k < 2 ? lo : hi;
+    if constexpr (__is_same(S, bf16)) {
+      const bf16x2 x = k & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true)
+                             : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false);
+      r[2 * k] = x[0]; r[2 * k + 1] = x[1];
+    } else {
+      const f16x2 x = k & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true)
+                            : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false);
+      r[2 * k] = x[0]; r[2 * k + 1] = x[1];
+    }
+  }
+  return r;
+}
+
+// A wave's place in the list of tiles: tile j of the nt of unit u of sequence b.
+struct Place {
+  int b, u, j, nt, len, bad;
+};
+
+template <typename S, typename C, int HD>
+__global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
+  using T = Tile<C, HD>;
+  constexpr bool F32 = sizeof(C) == 4, F8 = sizeof(C) == 1;
+  constexpr int KT = T::KT, KB = KT / 16, FT = HD / 16, NT = T::NT, ND = 2 * T::NI;
+  __shared__ __align__(1024) uint8_t kv[2][2][KT * T::RB];     // [stage][K, V]
+  __shared__ int pg[4][NT * 64];                               // pages of a tile's rows
+  __shared__ int s_len[KRAKEN_MAX_SEQS];                       // keys, -1: out of range
+
+  const int lane = threadIdx.x, w = blockIdx.x, g = lane >> 4, col = lane & 15;
+  const int B = p.cache.seqs, U = p.cache.n * p.cache.heads * p.qblocks;
+
+  // lengths, and the tiles of sequences 0 .. b for the lane's four
+  int64_t total;
+  int incl[4];
+  {
+    int sum = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int b = lane * 4 + e;
+      int len = b < B ? p.lens[b] : 0;
+      if (len < 0 || len > p.max_len) len = -1;
+      s_len[b] = len;
+      sum += len > 0 ? (len + KT - 1) / KT : 0;
+      incl[e] = sum;
+    }
+    int scan = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int up = __shfl_up(scan, d, 64);
+      if (lane >= d) scan += up;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) incl[e] += scan - sum;
+    total = (int64_t)uniform(__shfl(scan, 63, 64)) * U;
+  }
+  auto len_of = [&](int b) { return uniform(s_len[b]); };
+
+  // rows without keys: zeros, or NaN for a length out of range
+  for (int r = w; r < p.cache.n * B; r += gridDim.x) {
+    const int i = r / B, b = r % B, len = len_of(b);
+    if (len > 0) continue;
+    if (len < 0 && p.fault && lane == 0) *p.fault = 1;
+    S* out = static_cast<S*>(p.out.data) + i * p.out.sub + b * p.out.row;
+    for (int c = lane; c < p.heads * HD; c += 64) out[c] = len < 0 ? (S)NAN : (S)0.f;
+  }
+
+  const int W = (int)(total < p.W ? total : p.W);              // waves with work
+  if (p.desc && lane == 0) p.desc[w] = make_int4(0, 0, 0, 0);
+  if (w >= W) return;
+  const int64_t begin = split_begin(total, W, w);
+  const int cnt = (int)(split_begin(total, W, w + 1) - begin);
+
+  Place tp;                                                    // of the next tile to look up
+  {
+    const int x = (int)(begin / U);
+    int b = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) b += __popcll(__ballot(incl[e] <= x));
+    b = uniform(b);
+    tp.b = b;
+    tp.len = len_of(b);
+    tp.nt = (tp.len + KT - 1) / KT;
+    // tiles before b: its own inclusive count less its tiles
+    const int own = (b & 3) == 0 ? incl[0] : (b & 3) == 1 ? incl[1] : (b & 3) == 2 ? incl[2] : incl[3];
+    const int64_t rem = begin - (int64_t)(uniform(__shfl(own, b >> 2, 64)) - tp.nt) * U;
+    tp.u = (int)(rem / tp.nt);
+    tp.j = (int)(rem - (int64_t)tp.u * tp.nt);
+    tp.bad = 0;
+  }
+  auto advance = [&](Place& c) {
+    if (++c.j < c.nt) return;
+    c.j = 0;
+    if (++c.u < U) return;
+    c.u = 0;
+    do ++c.b; while (c.b < B - 1 && len_of(c.b) <= 0);
+    c.len = len_of(min(c.b, B - 1));
+    c.nt = (c.len + KT - 1) / KT;
+  };
+
+  const int64_t page_bytes = (int64_t)p.cache.heads * p.cache.page.d * T::RB;
+  const int64_t v_off = p.cache.pages * page_bytes;
+  // page numbers of a tile's rows; rows behind the last key are the last key's
+  auto look_up = [&](const Place& c, int slot) {
+    const int32_t* row = p.cache.table + (int64_t)c.b * p.cache.table_ld;
+#pragma unroll
+    for (int x = 0; x < NT; ++x) {
+      const int key = min(c.j * KT + x * 64 + lane, c.len - 1);
+      dma4(lds_addr(&pg[slot][x * 64]), row + div_of(p.cache.page, (uint32_t)key));
+    }
+  };
+  auto fetch = [&](Place& c, int slot, int stage) {
+    const int hq = c.u / p.qblocks, i = hq / p.cache.heads, h = hq % p.cache.heads;
+    const uint8_t* base = static_cast<const uint8_t*>(p.cache.data) +
+                          2 * i * v_off + (int64_t)h * p.cache.page.d * T::RB;
+    bool bad = false;
+#pragma unroll
+    for (int x = 0; x < T::NI; ++x) {
+      const int r = x * T::RPI + lane / T::NC, key = min(c.j * KT + r, c.len - 1);
+      const int place = key - (int)(div_of(p.cache.page, (uint32_t)key) * p.cache.page.d);
+      int page = pg[slot][r];
+      const bool ok = page >= 0 && page < p.cache.pages;
+      bad |= !ok;
+      page = ok ? page : 0;
+      const uint8_t* at = base + (uint64_t)(uint32_t)page * (uint32_t)page_bytes +
+                          (uint32_t)(place * T::RB);
+      const int pc = lane % T::NC;
+      dma16(lds_addr(&kv[stage][0][x * 1024]), at + (pc ^ k_key<C, HD>(r)) * 16);
+      dma16(lds_addr(&kv[stage][1][x * 1024]), at + v_off + (pc ^ v_key<C, HD>(r)) * 16);
+    }
+    c.bad = __any(bad);
+  };
+
+  // state of the unit at hand: the lane's query head col
+  Vec8<typename std::conditional<F32, f16, S>::type> q[F32 ? 1 : HD / 32];
+  f32x4 q4[F32 ? HD / 16 : 1];
+  f32x4 acc[FT];
+  float m_run = -INFINITY, l_run = 0.f, ks = 0.f, vs = 1.f;
+  int i = 0, h = 0, h0 = 0, nh = 0, bad = 0;
+  bool began = false;
+
+  auto open_unit = [&](const Place& c) {
+    const int hq = c.u / p.qblocks, qb = c.u % p.qblocks;
+    i = hq / p.cache.heads;
+    h = hq % p.cache.heads;
+    h0 = h * p.group + qb * 16;
+    nh = min(16, p.group - qb * 16);
+    const S* src = static_cast<const S*>(p.q.data) + i * p.q.sub + c.b * p.q.row +
+                   (int64_t)(h0 + min(col, nh - 1)) * HD;
+    const bool mine = col < nh;
+    if constexpr (F32) {
+#pragma unroll
+      for (int m = 0; m < HD / 16; ++m) {
+        q4[m] = *reinterpret_cast<const f32x4*>(src + 16 * m + 4 * g);
+        if (!mine) q4[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+    } else {
+#pragma unroll
+      for (int m = 0; m < HD / 32; ++m) {
+        // dimensions of k slot 8 g + e of product m: as the K operand's
+        const int at = F8 && HD > 32 ? 64 * (m / 2) + 16 * g + 8 * (m % 2) : 32 * m + 8 * g;
+        uint4 v = *reinterpret_cast<const uint4*>(src + at);
+        if (!mine) v = make_uint4(0, 0, 0, 0);
+        q[m] = __builtin_bit_cast(Vec8<S>, v);
+      }
+    }
+    ks = p.scale * 1.44269504088896341f;
+    vs = 1.f;
+    if constexpr (F8) {
+      ks *= p.cache.scales[(i * 2) * p.cache.heads + h];
+      vs = p.cache.scales[(i * 2 + 1) * p.cache.heads + h];
+    }
+    m_run = -INFINITY;
+    l_run = 0.f;
+    bad = 0;
+    began = c.j == 0;
+#pragma unroll
+    for (int f = 0; f < FT; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
+  };
+
+  auto compute = [&](const Place& c, int stage) {
+    const uint8_t* K = kv[stage][0];
+    const uint8_t* V = kv[stage][1];
+    f32x4 sc[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const int r = kb * 16 + col;
+      const uint8_t* row = K + r * T::RB;
+      const int key = k_key<C, HD>(r);
+      sc[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (F32) {
+#pragma unroll
+        for (int m = 0; m < HD / 16; ++m) {
+          const f32x4 a = *reinterpret_cast<const f32x4*>(row + ((4 * m + g) ^ key) * 16);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            sc[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], q4[m][e], sc[kb], 0, 0, 0);
+        }
+      } else if constexpr (F8 && HD == 32) {
+        const uint2 a = *reinterpret_cast<const uint2*>(row + ((g / 2) ^ key) * 16 + g % 2 * 8);
+        sc[kb] = mfma32<S>(from_e4m3<S>(a.x, a.y), q[0], sc[kb]);
+      } else if constexpr (F8) {
+#pragma unroll
+        for (int m = 0; m < HD / 64; ++m) {
+          const uint4 a = *reinterpret_cast<const uint4*>(row + ((4 * m + g) ^ key) * 16);
+          sc[kb] = mfma32<S>(from_e4m3<S>(a.x, a.y), q[2 * m], sc[kb]);
+          sc[kb] = mfma32<S>(from_e4m3<S>(a.z, a.w), q[2 * m + 1], sc[kb]);
+        }
+      } else {
+#pragma unroll
+        for (int m = 0; m < HD / 32; ++m) {
+          const uint4 a = *reinterpret_cast<const uint4*>(row + ((4 * m + g) ^ key) * 16);
+          sc[kb] = mfma32<S>(__builtin_bit_cast(Vec8<S>, a), q[m], sc[kb]);
+        }
+      }
+    }
+    // scores in base-2 units, of keys 16 kb + 4 g + r
+    const int left = c.len - c.j * KT;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float s = sc[kb][r] * ks;
+        if (left < KT && kb * 16 + 4 * g + r >= left) s = -INFINITY;
+        sc[kb][r] = s;
+        mx = fmaxf(mx, s);
+      }
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    if (__any(mx > m_run)) {
+      const float m_new = fmaxf(m_run, mx);
+      // (a head without a finite score yet has sums of zero, which any factor but NaN keeps)
+      const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
+      l_run *= alpha;
+#pragma unroll
+      for (int f = 0; f < FT; ++f)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[f][r] *= alpha;
+      m_run = m_new;
+    }
+    const float mref = m_run == -INFINITY ? 0.f : m_run;
+    float ps = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        sc[kb][r] = __builtin_amdgcn_exp2f(sc[kb][r] - mref);
+        ps += sc[kb][r];
+      }
+    l_run += ps;                              // of the lane's keys; the lanes join at the end
+    if constexpr (F32) {
+      constexpr int E = HD < 64 ? 2 : 4;      // features 16 E cc + E row + e of one LDS read
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const uint8_t* row = V + (kb * 16 + 4 * g + r) * T::RB;
+#pragma unroll
+          for (int cc = 0; cc < FT / E; ++cc) {
+            typedef float vec __attribute__((ext_vector_type(E)));
+            const vec v = *reinterpret_cast<const vec*>(row + (cc * 16 + col) * 4 * E);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+              acc[cc * E + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], sc[kb][r],
+                                                                     acc[cc * E + e], 0, 0, 0);
+          }
+        }
+    } else {
+#pragma unroll
+      for (int k2 = 0; k2 < KB / 2; ++k2) {
+        // k slots 8 g + e: keys 4 g + e of block 2 k2, then of the next.  A weight goes into
+        // the product as two terms, its rounding to S and what that leaves out: the output
+        // keeps 16 bits of it and more, and the second product is free next to the loads.
+        Vec8<S> hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float x = sc[2 * k2 + e / 4][e % 4];
+          hi[e] = (S)x;
+          lo[e] = (S)(x - (float)hi[e]);
+        }
+#pragma unroll
+        for (int f = 0; f < FT; ++f) {
+          Vec8<S> a;
+          if constexpr (F8) {
+            const int e = col / 2, r = k2 * 32 + 16 * (e / 4) + 4 * g + e % 4;
+            const i32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                (__attribute__((address_space(3))) i32x2*)(
+                    V + r * T::RB + (f ^ v_key<C, HD>(r)) * 16 + (col & 1) * 8));
+            a = from_e4m3<S>((uint32_t)x[0], (uint32_t)x[1]);
+          } else {
+            s16x4 x[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int r = k2 * 32 + 16 * e + 4 * g + col / 4;
+              x[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                  (__attribute__((address_space(3))) s16x4*)(
+                      V + r * T::RB + ((2 * f + (col & 3) / 2) ^ v_key<C, HD>(r)) * 16 +
+                      (col & 1) * 8));
+            }
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            const s16x8 both = __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
+            a = __builtin_bit_cast(Vec8<S>, both);
+          }
+          acc[f] = mfma32<S>(a, hi, acc[f]);
+          acc[f] = mfma32<S>(a, lo, acc[f]);
+        }
+      }
+    }
+    bad |= c.bad;
+  };
+
+  // four neighbouring features of the lane's query head, the n-th of HD / 16 times, and the
+  // first of them
+  auto four = [&](int n, int& feature) {
+    if constexpr (F32 && HD == 32) {
+      feature = 8 * g + 4 * n;
+      return f32x4{acc[0][2 * n], acc[1][2 * n], acc[0][2 * n + 1], acc[1][2 * n + 1]};
+    } else if constexpr (F32) {
+      const int cc = n / 4, r = n % 4;
+      feature = 64 * cc + 16 * g + 4 * r;
+      return f32x4{acc[4 * cc][r], acc[4 * cc + 1][r], acc[4 * cc + 2][r], acc[4 * cc + 3][r]};
+    } else {
+      feature = 16 * n + 4 * g;
+      return acc[n];
+    }
+  };
+
+  // end of the unit (done) or of the wave's run in the middle of it
+  auto close_unit = [&](const Place& c, int64_t at) {
+    const bool done = c.j == c.nt - 1;
+    float l = l_run;
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (bad) {
+      l = NAN;
+      if (p.fault && lane == 0) *p.fault = 1;
+    }
+    if (began && done) {
+      if (col < nh) {
+        S* out = static_cast<S*>(p.out.data) + i * p.out.sub + c.b * p.out.row +
+                 (int64_t)(h0 + col) * HD;
+        const float inv = vs / l;
+#pragma unroll
+        for (int n = 0; n < FT; ++n) {
+          int feature;
+          const f32x4 v = four(n, feature);
+          typedef S S4 __attribute__((ext_vector_type(4)));
+          S4 x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = (S)(v[e] * inv);
+          *reinterpret_cast<S4*>(out + feature) = x;
+        }
+      }
+      return;
+    }
+    const int slot = 2 * w + (began ? 1 : 0);
+    if (began && lane == 0) {
+      const int last = split_last(total, W, at + (c.nt - 1 - c.j));
+      p.desc[w] = make_int4(last - w + 1, c.b, c.u, 0);
+    }
+    if (col < nh) {
+      if (g == 0) {
+        float* ml = p.ml + ((int64_t)slot * p.qh + col) * 2;
+        ml[0] = m_run;
+        ml[1] = l;
+      }
+      float* o = p.o + ((int64_t)slot * p.qh + col) * HD;
+#pragma unroll
+      for (int n = 0; n < FT; ++n) {
+        int feature;
+        const f32x4 v = four(n, feature);
+        *reinterpret_cast<f32x4*>(o + feature) = v;
+      }
+    }
+  };
+
+  // The run.  Memory operations in order: pages of tiles 0 and 1, then rows of tile t and pages
+  // of tile t + 2, tile after tile; while tile t is computed, the rows of t + 1 and the pages of
+  // t + 2 and t + 3 may be outstanding.
+  Place cur, nxt, tp2;                       // tiles t, t + 1 and t + 2
+  cur = tp;
+  look_up(tp, 0);
+  advance(tp);
+  nxt = tp;
+  if (cnt > 1) {
+    look_up(tp, 1);
+    advance(tp);
+  }
+  tp2 = tp;
+  wait_vm<0>();
+  fetch(cur, 0, 0);
+  if (cnt > 2) {
+    look_up(tp, 2);
+    advance(tp);
+  }
+  if (cnt > 1) fetch(nxt, 1, 1);
+  if (cnt > 3) {
+    look_up(tp, 3);
+  }
+  Place tp3 = tp;                            // tile t + 3
+  for (int t = 0; t < cnt; ++t) {
+    const int rem = cnt - t;
+    if (t == 0 || cur.j == 0) open_unit(cur);
+    if (rem > 3) wait_vm<ND + 2 * NT>();
+    else if (rem == 3) wait_vm<ND + NT>();
+    else if (rem == 2) wait_vm<ND>();
+    else wait_vm<0>();
+    compute(cur, t & 1);
+    if (cur.j == cur.nt - 1 || rem == 1) close_unit(cur, begin + t);
+    cur = nxt;
+    nxt = tp2;
+    if (rem > 2) {
+      // the stage's reads are done, and the page numbers are there
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (rem > 3) wait_vm<ND + NT>();
+      else wait_vm<ND>();
+      fetch(nxt, (t + 2) & 3, t & 1);
+      tp2 = tp3;
+      if (rem > 4) {
+        advance(tp3);
+        look_up(tp3, t & 3);
+      }
+    }
   }
 }
 
-// Block (head, sequence, sub-layer), 4 waves.  HD / 8 lanes take one key; every group of lanes
-// keeps the running maximum, sum and output of its keys, which are joined at the end.
-template <typename S, typename C, int HD>
-__global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnParams p) {
-  constexpr int L = HD / 8, KEYS = 256 / L;
-  __shared__ float sm[KEYS], sl[KEYS], so[KEYS][HD];
-  const int h = blockIdx.x, b = blockIdx.y, i = blockIdx.z, tid = threadIdx.x;
-  const int hkv = h / p.group, c = tid % L, g = tid / L;
-  S* out = static_cast<S*>(p.out.data) + i * p.out.sub + b * p.out.row + h * HD;
-  const int len = p.lens[b];
-  bool bad = len < 0 || len > p.max_len;
-  float q[8], o[8] = {}, m = -INFINITY, l = 0.f;
-  load8(static_cast<const S*>(p.q.data) + i * p.q.sub + b * p.q.row + h * HD + c * 8, q);
-  float ks = 1.f, vs = 1.f;
-  if (sizeof(C) == 1) {
-    ks = p.cache.scales[(i * 2) * p.cache.heads + hkv];
-    vs = p.cache.scales[(i * 2 + 1) * p.cache.heads + hkv];
-  }
-  for (int k = g; k < len && !bad; k += KEYS) {
-    const int page = paged_page(p.cache, b, k);
-    if (page < 0) {
-      bad = true;
-      break;
+// Joins the partials of the unit that begins in run w and ends in a later one: with M the
+// largest maximum, out = sum o e^(m - M) / sum l e^(m - M).  A group of HD / 4 lanes takes a
+// query head's partials, every LPH-th of them where there are more groups than heads.
+template <typename S, int HD>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p) {
+  constexpr int LQ = HD / 4, NG = 256 / LQ;
+  __shared__ float sm[NG], sl[NG];
+  __shared__ f32x4 so[NG][LQ];
+  const int w = blockIdx.x, tid = threadIdx.x, grp = tid / LQ, f = tid % LQ;
+  const int4 d = p.desc[w];
+  const int parts = d.x;
+  if (parts == 0) return;
+  const int b = d.y, u = d.z, hq = u / p.qblocks, qb = u % p.qblocks;
+  const int i = hq / p.cache.heads, h = hq % p.cache.heads;
+  const int h0 = h * p.group + qb * 16, nh = min(16, p.group - qb * 16);
+  const float vs = p.cache.scales ? p.cache.scales[(i * 2 + 1) * p.cache.heads + h] : 1.f;
+  // groups per head: a power of two
+  int gph = 1;
+  while (2 * gph * nh <= NG) gph *= 2;
+  for (int hb = 0; hb < nh; hb += NG / gph) {
+    const int head = hb + grp / gph, sub = grp % gph;
+    float m = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    if (head < nh) {
+      for (int k = sub; k < parts; k += gph) {
+        const int64_t slot = ((int64_t)(w + k) * 2 + (k == 0 ? 1 : 0)) * p.qh + head;
+        const float mk = p.ml[slot * 2], lk = p.ml[slot * 2 + 1];
+        const f32x4 ok = *reinterpret_cast<const f32x4*>(p.o + slot * HD + 4 * f);
+        const float mn = fmaxf(m, mk), ref = mn == -INFINITY ? 0.f : mn;
+        const float a = __builtin_amdgcn_exp2f(m - ref), c = __builtin_amdgcn_exp2f(mk - ref);
+        l = l * a + lk * c;
+        o = o * a + ok * c;
+        m = mn;
+      }
     }
-    const int place = k - (int)div_of(p.cache.page, (uint32_t)k) * (int)p.cache.page.d;
-    float x[8];
-    const C* data = static_cast<const C*>(p.cache.data);
-    load8(data + (paged_row(p.cache, i, 0, page, hkv) + place) * HD + c * 8, x);
-    float s = 0.f;
+    if (gph > 1) {
+      if (f == 0) {
+        sm[grp] = m;
+        sl[grp] = l;
+      }
+      so[grp][f] = o;
+      __syncthreads();
+      if (sub == 0) {
+        for (int k = 1; k < gph; ++k) {
+          const float mk = sm[grp + k], mn = fmaxf(m, mk), ref = mn == -INFINITY ? 0.f : mn;
+          const float a = __builtin_amdgcn_exp2f(m - ref), c = __builtin_amdgcn_exp2f(mk - ref);
+          l = l * a + sl[grp + k] * c;
+          o = o * a + so[grp + k][f] * c;
+          m = mn;
+        }
+      }
+      __syncthreads();
+    }
+    if (head < nh && sub == 0) {
+      S* out = static_cast<S*>(p.out.data) + i * p.out.sub + b * p.out.row +
+               (int64_t)(h0 + head) * HD + 4 * f;
+      typedef S S4 __attribute__((ext_vector_type(4)));
+      const float inv = vs / l;
+      S4 x;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s = fmaf(q[e], x[e], s);
-#pragma unroll
-    for (int w = 1; w < L; w <<= 1) s += __shfl_xor(s, w, 64);
-    s *= p.scale * ks;
-    const float mn = fmaxf(m, s), ref = mn == -INFINITY ? 0.f : mn;
-    const float alpha = __expf(m - ref), e1 = __expf(s - ref);
-    load8(data + (paged_row(p.cache, i, 1, page, hkv) + place) * HD + c * 8, x);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = o[e] * alpha + e1 * x[e];
-    l = l * alpha + e1;
-    m = mn;
+      for (int e = 0; e < 4; ++e) x[e] = (S)(o[e] * inv);
+      *reinterpret_cast<S4*>(out) = x;
+    }
   }
-  if (c == 0) {
-    sm[g] = m;
-    sl[g] = l;
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) so[g][c * 8 + e] = o[e];
-  bad = __syncthreads_or(bad);
-  if (bad && tid == 0 && p.fault) *p.fault = 1;
-  if (tid >= HD) return;
-  float M = -INFINITY, sum = 0.f, v = 0.f;
-  for (int k = 0; k < KEYS; ++k) M = fmaxf(M, sm[k]);
-  for (int k = 0; k < KEYS; ++k) {
-    const float w = sm[k] == -INFINITY ? 0.f : __expf(sm[k] - M);
-    sum += sl[k] * w;
-    v += so[k][tid] * w;
-  }
-  out[tid] = bad ? (S)NAN : len == 0 ? (S)0.f : (S)(v * vs / sum);
+}
+
+// Keys per tile of a cache with rows of head_dim elements of es bytes.
+int tile_keys(int head_dim, int es) { return std::min(128, 8192 / (head_dim * es)); }
+
+int cache_es(int dtype) {
+  return dtype == KRAKEN_DTYPE_E4M3 ? 1 : dtype == KRAKEN_DTYPE_F32 ? 4 : 2;
+}
+
+// Waves of a call: at most one per tile, and four per CU of the GPU's 256, one per SIMD, as many
+// as LDS holds.
+constexpr int MAX_WAVES = 1024;
+int waves_of(const kraken_paged_cache* c, int n_heads, int max_len) {
+  const int kt = tile_keys(c->head_dim, cache_es(c->dtype));
+  const int64_t units = (int64_t)c->n_sub * c->n_kv_heads * ((n_heads / c->n_kv_heads + 15) / 16);
+  const double tiles = (double)units * c->num_seqs * ((max_len + (int64_t)kt - 1) / kt);
+  return tiles >= MAX_WAVES ? MAX_WAVES : std::max(1, (int)tiles);
+}
+
+template <typename S, typename C, int HD>
+hipError_t launch_hd(const PagedAttnParams& p, hipStream_t s) {
+  hipLaunchKernelGGL((paged_attn_kernel<S, C, HD>), dim3((unsigned)p.W), dim3(64), 0, s, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.desc) return e;
+  hipLaunchKernelGGL((paged_join_kernel<S, HD>), dim3((unsigned)p.W), dim3(256), 0, s, p);
+  return hipGetLastError();
 }
 
 template <typename S, typename C>
 hipError_t launch_typed(const PagedAttnParams& p, int hd, hipStream_t s) {
-  const dim3 grid((unsigned)p.heads, (unsigned)p.cache.seqs, (unsigned)p.cache.n);
-  if (hd == 32) hipLaunchKernelGGL((paged_attn_kernel<S, C, 32>), grid, dim3(256), 0, s, p);
-  else if (hd == 64) hipLaunchKernelGGL((paged_attn_kernel<S, C, 64>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((paged_attn_kernel<S, C, 128>), grid, dim3(256), 0, s, p);
-  return hipGetLastError();
+  if (hd == 32) return launch_hd<S, C, 32>(p, s);
+  if (hd == 64) return launch_hd<S, C, 64>(p, s);
+  return launch_hd<S, C, 128>(p, s);
 }
 
 kraken_status fail(kraken_status s, const char* msg) { return (kraken_status)set_error(s, msg); }
@@ -128,7 +667,11 @@ int64_t kraken_paged_attention_work_floats(const kraken_paged_cache* cache, int3
       n_heads % cache->n_kv_heads != 0 || max_len < 0 ||
       max_len > (int64_t)cache->pages_per_seq * cache->page_size)
     return -1;
-  return 0;
+  // a unit of one tile is never split
+  if (max_len <= tile_keys(cache->head_dim, cache_es(cache->dtype))) return 0;
+  const int64_t W = waves_of(cache, n_heads, max_len);
+  const int64_t qh = std::min(16, n_heads / cache->n_kv_heads);
+  return W * (4 + 2 * qh * (2 + cache->head_dim));
 }
 
 kraken_status kraken_op_paged_attention(int32_t dtype, const kraken_rows* q,
@@ -150,13 +693,16 @@ kraken_status kraken_op_paged_attention(int32_t dtype, const kraken_rows* q,
     return fail(KRAKEN_ERR_INVALID_ARG, "n_kv_heads does not divide n_heads");
   if (max_len < 0 || max_len > (int64_t)cache->pages_per_seq * cache->page_size)
     return fail(KRAKEN_ERR_INVALID_ARG, "max_len out of 0..pages_per_seq * page_size");
+  if ((int64_t)cache->num_seqs * max_len >= (1ll << 35))
+    return fail(KRAKEN_ERR_UNSUPPORTED, "num_seqs * max_len must stay below 2^35");
   if (!isfinite(scale)) return fail(KRAKEN_ERR_INVALID_ARG, "scale is not finite");
   const int es = dtype == KRAKEN_DTYPE_F32 ? 4 : 2;
   for (const kraken_rows* r : {q, out})
     if (const char* msg = check_rows(r, cache->n_sub, cache->num_seqs, es,
                                      r == out ? (int64_t)n_heads * cache->head_dim : 0))
       return fail(KRAKEN_ERR_INVALID_ARG, msg);
-  if (work_floats < 0 || work_floats < kraken_paged_attention_work_floats(cache, n_heads, max_len))
+  const int64_t need = kraken_paged_attention_work_floats(cache, n_heads, max_len);
+  if (work_floats < need || (need > 0 && !work) || work_floats < 0)
     return fail(KRAKEN_ERR_INVALID_ARG, "work is smaller than the call needs");
   if (reinterpret_cast<uintptr_t>(work) % 16 != 0)
     return fail(KRAKEN_ERR_INVALID_ARG, "work is not 16-byte aligned");
@@ -165,6 +711,16 @@ kraken_status kraken_op_paged_attention(int32_t dtype, const kraken_rows* q,
   p.out = {out->data, out->sub_stride, out->row_stride};
   p.lens = lens; p.fault = fault;
   p.heads = n_heads; p.group = n_heads / cache->n_kv_heads; p.max_len = max_len;
+  p.qblocks = (p.group + 15) / 16;
+  p.qh = std::min(16, p.group);
+  p.W = waves_of(cache, n_heads, max_len);
+  p.desc = nullptr;
+  p.ml = p.o = nullptr;
+  if (need > 0) {
+    p.desc = reinterpret_cast<int4*>(work);
+    p.ml = work + 4 * (int64_t)p.W;
+    p.o = p.ml + 4 * (int64_t)p.W * p.qh;
+  }
   p.scale = scale != 0.f ? scale : (float)(1.0 / sqrt((double)hd));
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e;

@@ -1,0 +1,81 @@
+// The index arithmetic of the paged-cache kernels on the host: division by a page size, where a
+// position lies (bad pages, sequences and positions among them), and the equal runs of a list
+// of tiles.  Exits 0 when every result is the plain computation's.
+#include <cstdio>
+#include <cstdlib>
+#include <random>
+#include <vector>
+
+#include "../paper_2408_07802_amd/csrc/paged.hpp"
+
+using namespace kraken;
+
+#define CHECK(x)                                                \
+  do {                                                          \
+    if (!(x)) {                                                 \
+      std::fprintf(stderr, "line %d: %s\n", __LINE__, #x);      \
+      std::exit(1);                                             \
+    }                                                           \
+  } while (0)
+
+int main() {
+  std::mt19937_64 rng(1);
+  // division: small and large divisors, powers of two and their neighbours
+  std::vector<uint32_t> divisors{1, 2, 3, 5, 7, 16, 48, 4099, (1u << 31) - 1};
+  for (int l = 2; l < 31; ++l)
+    for (int k = -1; k <= 1; ++k) divisors.push_back((1u << l) + k);
+  for (uint32_t d : divisors) {
+    const FastDiv f = fast_div(d);
+    for (int k = 0; k < 2000; ++k) {
+      uint32_t x = (uint32_t)(rng() >> (33 + rng() % 31));
+      if (k % 3 == 0) x = (uint32_t)((uint64_t)x * d & 0x7fffffff) / d * d;   // multiples
+      if (k % 3 == 1 && x >= d) x = x / d * d - 1;                            // and one less
+      CHECK(div_of(f, x) == x / d);
+    }
+    CHECK(div_of(f, 0x7fffffffu) == 0x7fffffffu / d);
+  }
+
+  // positions: the table is exactly as large as said (the sanitizer sees a read past it)
+  for (int k = 0; k < 500; ++k) {
+    PagedView c{};
+    c.seqs = 1 + (int)(rng() % 4);
+    c.per_seq = 1 + (int)(rng() % 6);
+    c.table_ld = c.per_seq + (int)(rng() % 3);
+    c.pages = 1 + (int)(rng() % 10);
+    c.page = fast_div(1 + (uint32_t)(rng() % 40));
+    std::vector<int32_t> table((size_t)(c.seqs - 1) * c.table_ld + c.per_seq);
+    for (auto& e : table) e = (int32_t)(rng() % (c.pages + 4)) - 2;
+    c.table = table.data();
+    const int ps = (int)c.page.d;
+    for (int b = -2; b < c.seqs + 2; ++b)
+      for (int pos : {0, 1, ps - 1, ps, c.per_seq * ps - 1, c.per_seq * ps, 0x7fffffff}) {
+        int want = -1;
+        if (b >= 0 && b < c.seqs && pos / ps < c.per_seq) {
+          const int page = table[(size_t)b * c.table_ld + pos / ps];
+          if (page >= 0 && page < c.pages) want = page;
+        }
+        CHECK(paged_page(c, b, pos) == want);
+      }
+  }
+
+  // runs: every item in one run, run lengths that differ by at most one, and the last run of
+  // an item
+  for (int k = 0; k < 3000; ++k) {
+    const int64_t total = 1 + (int64_t)(rng() % (k % 2 ? 5000 : 60));
+    const int runs = (int)(1 + rng() % (total < 1024 ? total : 1024));
+    CHECK(split_begin(total, runs, 0) == 0 && split_begin(total, runs, runs) == total);
+    for (int w = 0; w < runs; ++w) {
+      const int64_t a = split_begin(total, runs, w), e = split_begin(total, runs, w + 1);
+      CHECK(e - a >= total / runs && e - a <= (total + runs - 1) / runs && e > a);
+      for (int64_t item = a; item < e; ++item) CHECK(split_last(total, runs, item) == w);
+    }
+  }
+  // (a list as long as a call can have: 2^31 tiles of 2^24 units)
+  const int64_t big = (1ll << 31) * (1ll << 21);
+  for (int w = 0; w < 1024; ++w) {
+    const int64_t a = split_begin(big, 1024, w);
+    CHECK(split_last(big, 1024, a) == w && (w == 0 || split_last(big, 1024, a - 1) == w - 1));
+  }
+  std::puts("paged index arithmetic holds");
+  return 0;
+}

@@ -3,6 +3,9 @@ the device is touched (these run without one), and sizes are what the header say
 
 import ctypes
 import math
+import os
+import shutil
+import subprocess
 
 import pytest
 import torch
@@ -203,3 +206,18 @@ def test_binding_refuses_wrong_tensors(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
     with pytest.raises(ValueError, match="current device"):
         K.op_paged_append(q, kv, kv, pages, table, i3, q)
+
+
+# -------------------------------------------------------- the kernels' index arithmetic, on the host
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="no host compiler")
+def test_index_arithmetic_under_the_sanitizers(tmp_path):
+    src = os.path.join(os.path.dirname(os.path.abspath(__file__)), "paged_driver.cpp")
+    exe = str(tmp_path / "driver")
+    res = subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=address,undefined",
+                          "-fno-sanitize-recover=all", src, "-o", exe],
+                         capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr[-3000:]
+    res = subprocess.run([exe], capture_output=True, text=True, timeout=120,
+                         env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"))
+    assert res.returncode == 0 and "holds" in res.stdout, res.stdout + res.stderr[-3000:]
