@@ -40,11 +40,13 @@ struct PagedAttnParams {
   PagedView cache;
   const int32_t* lens;
   int32_t* fault;
-  int4* desc;           // [W]: units that begin in a run and do not end there (parts, b, u, 0)
+  int4* desc;           // units that runs share (parts, first run, b, u): see desc_at
   float* ml;            // [W][2][qh][2]: maximum and sum
   float* o;             // [W][2][qh][HD]: unnormalised output
   int heads, group, max_len, W;
   int qblocks, qh;      // blocks of query heads per key/value head; query heads per block (<= 16)
+  int whole;            // runs end where units end: nothing is shared
+  int by_unit;          // desc has an entry per unit (of every sequence), not per run
   float scale;
 };
 
@@ -140,10 +142,14 @@ __device__ __forceinline__ Vec8<S> from_e4m3(uint32_t lo, uint32_t hi) {
   return r;
 }
 
-// A wave's place in the list of tiles: tile j of the nt of unit u of sequence b.
+// A wave's place in the list of tiles: tile j of the nt of unit u (sub-layer i, key/value head
+// h, query block qb) of sequence b.
 struct Place {
-  int b, u, j, nt, len, bad;
+  int b, u, i, h, qb, j, nt, len, bad;
 };
+
+// Queries of a unit in LDS: rows of qh heads, in whole DMA instructions.
+constexpr int q_slot(int qh, int row_bytes) { return (qh * row_bytes + 1023) / 1024 * 1024; }
 
 template <typename S, typename C, int HD>
 __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
@@ -153,6 +159,7 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
   __shared__ __align__(1024) uint8_t kv[2][2][KT * T::RB];     // [stage][K, V]
   __shared__ int pg[4][NT * 64];                               // pages of a tile's rows
   __shared__ int s_len[KRAKEN_MAX_SEQS];                       // keys, -1: out of range
+  extern __shared__ __align__(16) uint8_t q_rows[];            // [2][q_slot]
 
   const int lane = threadIdx.x, w = blockIdx.x, g = lane >> 4, col = lane & 15;
   const int B = p.cache.seqs, U = p.cache.n * p.cache.heads * p.qblocks;
@@ -187,39 +194,60 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
   for (int r = w; r < p.cache.n * B; r += gridDim.x) {
     const int i = r / B, b = r % B, len = len_of(b);
     if (len > 0) continue;
+    if (p.by_unit)
+      for (int u = lane; u < p.cache.heads * p.qblocks; u += 64)
+        p.desc[b * U + i * p.cache.heads * p.qblocks + u] = make_int4(0, 0, 0, 0);
     if (len < 0 && p.fault && lane == 0) *p.fault = 1;
     S* out = static_cast<S*>(p.out.data) + i * p.out.sub + b * p.out.row;
     for (int c = lane; c < p.heads * HD; c += 64) out[c] = len < 0 ? (S)NAN : (S)0.f;
   }
 
   const int W = (int)(total < p.W ? total : p.W);              // waves with work
-  if (p.desc && lane == 0) p.desc[w] = make_int4(0, 0, 0, 0);
+  if (p.desc && !p.by_unit && lane == 0) p.desc[w] = make_int4(0, 0, 0, 0);
   if (w >= W) return;
-  const int64_t begin = split_begin(total, W, w);
-  const int cnt = (int)(split_begin(total, W, w + 1) - begin);
 
-  Place tp;                                                    // of the next tile to look up
-  {
-    const int x = (int)(begin / U);
+  // sequence, unit and tile of an item of the list
+  auto place_of = [&](int64_t item) {
+    Place c;
+    const int x = (int)(item / U);
     int b = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) b += __popcll(__ballot(incl[e] <= x));
     b = uniform(b);
-    tp.b = b;
-    tp.len = len_of(b);
-    tp.nt = (tp.len + KT - 1) / KT;
+    c.b = b;
+    c.len = len_of(b);
+    c.nt = (c.len + KT - 1) / KT;
     // tiles before b: its own inclusive count less its tiles
     const int own = (b & 3) == 0 ? incl[0] : (b & 3) == 1 ? incl[1] : (b & 3) == 2 ? incl[2] : incl[3];
-    const int64_t rem = begin - (int64_t)(uniform(__shfl(own, b >> 2, 64)) - tp.nt) * U;
-    tp.u = (int)(rem / tp.nt);
-    tp.j = (int)(rem - (int64_t)tp.u * tp.nt);
-    tp.bad = 0;
-  }
+    const int64_t rem = item - (int64_t)(uniform(__shfl(own, b >> 2, 64)) - c.nt) * U;
+    c.u = (int)(rem / c.nt);
+    c.j = (int)(rem - (int64_t)c.u * c.nt);
+    c.qb = c.u % p.qblocks;
+    c.h = c.u / p.qblocks % p.cache.heads;
+    c.i = c.u / p.qblocks / p.cache.heads;
+    c.bad = 0;
+    return c;
+  };
+  // an item, or the first behind its unit where it lies inside one and units are not shared
+  auto edge = [&](int64_t item) {
+    if (!p.whole || item == 0 || item == total) return item;
+    const Place c = place_of(item);
+    return c.j == 0 ? item : item + c.nt - c.j;
+  };
+  const int64_t begin = edge(split_begin(total, W, w));
+  const int cnt = (int)(edge(split_begin(total, W, w + 1)) - begin);
+  if (cnt == 0) return;
+  Place tp = place_of(begin);                                  // of the next tile to look up
   auto advance = [&](Place& c) {
     if (++c.j < c.nt) return;
     c.j = 0;
-    if (++c.u < U) return;
-    c.u = 0;
+    ++c.u;
+    if (++c.qb < p.qblocks) return;
+    c.qb = 0;
+    if (++c.h < p.cache.heads) return;
+    c.h = 0;
+    if (++c.i < p.cache.n) return;
+    c.i = c.u = 0;
     do ++c.b; while (c.b < B - 1 && len_of(c.b) <= 0);
     c.len = len_of(min(c.b, B - 1));
     c.nt = (c.len + KT - 1) / KT;
@@ -236,10 +264,20 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
       dma4(lds_addr(&pg[slot][x * 64]), row + div_of(p.cache.page, (uint32_t)key));
     }
   };
-  auto fetch = [&](Place& c, int slot, int stage) {
-    const int hq = c.u / p.qblocks, i = hq / p.cache.heads, h = hq % p.cache.heads;
+  // a tile's rows, behind the queries of a unit that begins with it
+  constexpr int RBQ = HD * (int)sizeof(S);
+  auto fetch = [&](Place& c, int slot, int stage, bool first) {
+    if (c.j == 0 || first) {             // a unit's queries, adjacent rows
+      const int qb16 = c.qb * 16, nh = min(16, p.group - qb16);
+      const uint8_t* src = reinterpret_cast<const uint8_t*>(
+          static_cast<const S*>(p.q.data) + c.i * p.q.sub + c.b * p.q.row +
+          (int64_t)(c.h * p.group + qb16) * HD);
+      const uint32_t to = lds_addr(q_rows) + stage * q_slot(p.qh, RBQ);
+      for (int x = 0; x < nh * RBQ; x += 1024)
+        dma16(to + x, src + min(x + lane * 16, nh * RBQ - 16));
+    }
     const uint8_t* base = static_cast<const uint8_t*>(p.cache.data) +
-                          2 * i * v_off + (int64_t)h * p.cache.page.d * T::RB;
+                          2 * c.i * v_off + (int64_t)c.h * p.cache.page.d * T::RB;
     bool bad = false;
 #pragma unroll
     for (int x = 0; x < T::NI; ++x) {
@@ -263,17 +301,14 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
   f32x4 q4[F32 ? HD / 16 : 1];
   f32x4 acc[FT];
   float m_run = -INFINITY, l_run = 0.f, ks = 0.f, vs = 1.f;
-  int i = 0, h = 0, h0 = 0, nh = 0, bad = 0;
+  int h0 = 0, nh = 0, bad = 0;
   bool began = false;
 
-  auto open_unit = [&](const Place& c) {
-    const int hq = c.u / p.qblocks, qb = c.u % p.qblocks;
-    i = hq / p.cache.heads;
-    h = hq % p.cache.heads;
-    h0 = h * p.group + qb * 16;
-    nh = min(16, p.group - qb * 16);
-    const S* src = static_cast<const S*>(p.q.data) + i * p.q.sub + c.b * p.q.row +
-                   (int64_t)(h0 + min(col, nh - 1)) * HD;
+  auto open_unit = [&](const Place& c, int stage) {
+    h0 = c.h * p.group + c.qb * 16;
+    nh = min(16, p.group - c.qb * 16);
+    const S* src = reinterpret_cast<const S*>(q_rows + stage * q_slot(p.qh, RBQ)) +
+                   min(col, nh - 1) * HD;
     const bool mine = col < nh;
     if constexpr (F32) {
 #pragma unroll
@@ -294,8 +329,8 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
     ks = p.scale * 1.44269504088896341f;
     vs = 1.f;
     if constexpr (F8) {
-      ks *= p.cache.scales[(i * 2) * p.cache.heads + h];
-      vs = p.cache.scales[(i * 2 + 1) * p.cache.heads + h];
+      ks *= p.cache.scales[(c.i * 2) * p.cache.heads + c.h];
+      vs = p.cache.scales[(c.i * 2 + 1) * p.cache.heads + c.h];
     }
     m_run = -INFINITY;
     l_run = 0.f;
@@ -464,8 +499,9 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
       if (p.fault && lane == 0) *p.fault = 1;
     }
     if (began && done) {
+      if (p.by_unit && lane == 0) p.desc[c.b * U + c.u] = make_int4(0, 0, 0, 0);
       if (col < nh) {
-        S* out = static_cast<S*>(p.out.data) + i * p.out.sub + c.b * p.out.row +
+        S* out = static_cast<S*>(p.out.data) + c.i * p.out.sub + c.b * p.out.row +
                  (int64_t)(h0 + col) * HD;
         const float inv = vs / l;
 #pragma unroll
@@ -484,7 +520,7 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
     const int slot = 2 * w + (began ? 1 : 0);
     if (began && lane == 0) {
       const int last = split_last(total, W, at + (c.nt - 1 - c.j));
-      p.desc[w] = make_int4(last - w + 1, c.b, c.u, 0);
+      p.desc[p.by_unit ? c.b * U + c.u : w] = make_int4(last - w + 1, w, c.b, c.u);
     }
     if (col < nh) {
       if (g == 0) {
@@ -516,23 +552,23 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
   }
   tp2 = tp;
   wait_vm<0>();
-  fetch(cur, 0, 0);
+  fetch(cur, 0, 0, true);
   if (cnt > 2) {
     look_up(tp, 2);
     advance(tp);
   }
-  if (cnt > 1) fetch(nxt, 1, 1);
+  if (cnt > 1) fetch(nxt, 1, 1, false);
   if (cnt > 3) {
     look_up(tp, 3);
   }
   Place tp3 = tp;                            // tile t + 3
   for (int t = 0; t < cnt; ++t) {
     const int rem = cnt - t;
-    if (t == 0 || cur.j == 0) open_unit(cur);
     if (rem > 3) wait_vm<ND + 2 * NT>();
     else if (rem == 3) wait_vm<ND + NT>();
     else if (rem == 2) wait_vm<ND>();
     else wait_vm<0>();
+    if (t == 0 || cur.j == 0) open_unit(cur, t & 1);
     compute(cur, t & 1);
     if (cur.j == cur.nt - 1 || rem == 1) close_unit(cur, begin + t);
     cur = nxt;
@@ -542,7 +578,7 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (rem > 3) wait_vm<ND + NT>();
       else wait_vm<ND>();
-      fetch(nxt, (t + 2) & 3, t & 1);
+      fetch(nxt, (t + 2) & 3, t & 1, false);
       tp2 = tp3;
       if (rem > 4) {
         advance(tp3);
@@ -552,39 +588,53 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
   }
 }
 
-// Joins the partials of the unit that begins in run w and ends in a later one: with M the
-// largest maximum, out = sum o e^(m - M) / sum l e^(m - M).  A group of HD / 4 lanes takes a
-// query head's partials, every LPH-th of them where there are more groups than heads.
+// Joins the partials of a unit that several runs share: with M the largest maximum,
+// out = sum o e^(m - M) / sum l e^(m - M).  Block (entry of desc, share of the query heads); a
+// group of HD / 4 lanes takes a query head's partials, every gph-th of them where there are more
+// groups than heads.
 template <typename S, int HD>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p) {
   constexpr int LQ = HD / 4, NG = 256 / LQ;
   __shared__ float sm[NG], sl[NG];
   __shared__ f32x4 so[NG][LQ];
-  const int w = blockIdx.x, tid = threadIdx.x, grp = tid / LQ, f = tid % LQ;
-  const int4 d = p.desc[w];
-  const int parts = d.x;
+  const int tid = threadIdx.x, grp = tid / LQ, f = tid % LQ;
+  const int4 d = p.desc[blockIdx.x];
+  const int parts = d.x, w = d.y, b = d.z, u = d.w;
   if (parts == 0) return;
-  const int b = d.y, u = d.z, hq = u / p.qblocks, qb = u % p.qblocks;
+  const int hq = u / p.qblocks, qb = u % p.qblocks;
   const int i = hq / p.cache.heads, h = hq % p.cache.heads;
   const int h0 = h * p.group + qb * 16, nh = min(16, p.group - qb * 16);
+  const int share = (p.qh + gridDim.y - 1) / gridDim.y, end = min(nh, (int)(blockIdx.y + 1) * share);
   const float vs = p.cache.scales ? p.cache.scales[(i * 2 + 1) * p.cache.heads + h] : 1.f;
   // groups per head: a power of two
   int gph = 1;
-  while (2 * gph * nh <= NG) gph *= 2;
-  for (int hb = 0; hb < nh; hb += NG / gph) {
+  while (2 * gph * share <= NG) gph *= 2;
+  for (int hb = blockIdx.y * share; hb < end; hb += NG / gph) {
     const int head = hb + grp / gph, sub = grp % gph;
     float m = -INFINITY, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    if (head < nh) {
-      for (int k = sub; k < parts; k += gph) {
-        const int64_t slot = ((int64_t)(w + k) * 2 + (k == 0 ? 1 : 0)) * p.qh + head;
-        const float mk = p.ml[slot * 2], lk = p.ml[slot * 2 + 1];
-        const f32x4 ok = *reinterpret_cast<const f32x4*>(p.o + slot * HD + 4 * f);
-        const float mn = fmaxf(m, mk), ref = mn == -INFINITY ? 0.f : mn;
-        const float a = __builtin_amdgcn_exp2f(m - ref), c = __builtin_amdgcn_exp2f(mk - ref);
-        l = l * a + lk * c;
-        o = o * a + ok * c;
-        m = mn;
+    auto merge = [&](float mk, float lk, f32x4 ok) {
+      const float mn = fmaxf(m, mk), ref = mn == -INFINITY ? 0.f : mn;
+      const float a = __builtin_amdgcn_exp2f(m - ref), c = __builtin_amdgcn_exp2f(mk - ref);
+      l = l * a + lk * c;
+      o = o * a + ok * c;
+      m = mn;
+    };
+    if (head < end) {
+      for (int k0 = sub; k0 < parts; k0 += 4 * gph) {          // four loads in flight
+        float mk[4], lk[4];
+        f32x4 ok[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int k = min(k0 + x * gph, parts - 1);
+          const int64_t slot = ((int64_t)(w + k) * 2 + (k == 0 ? 1 : 0)) * p.qh + head;
+          mk[x] = p.ml[slot * 2];
+          lk[x] = p.ml[slot * 2 + 1];
+          ok[x] = *reinterpret_cast<const f32x4*>(p.o + slot * HD + 4 * f);
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (k0 + x * gph < parts) merge(mk[x], lk[x], ok[x]);
       }
     }
     if (gph > 1) {
@@ -594,18 +644,11 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p) {
       }
       so[grp][f] = o;
       __syncthreads();
-      if (sub == 0) {
-        for (int k = 1; k < gph; ++k) {
-          const float mk = sm[grp + k], mn = fmaxf(m, mk), ref = mn == -INFINITY ? 0.f : mn;
-          const float a = __builtin_amdgcn_exp2f(m - ref), c = __builtin_amdgcn_exp2f(mk - ref);
-          l = l * a + sl[grp + k] * c;
-          o = o * a + so[grp + k][f] * c;
-          m = mn;
-        }
-      }
+      if (sub == 0)
+        for (int k = 1; k < gph; ++k) merge(sm[grp + k], sl[grp + k], so[grp + k][f]);
       __syncthreads();
     }
-    if (head < nh && sub == 0) {
+    if (head < end && sub == 0) {
       S* out = static_cast<S*>(p.out.data) + i * p.out.sub + b * p.out.row +
                (int64_t)(h0 + head) * HD + 4 * f;
       typedef S S4 __attribute__((ext_vector_type(4)));
@@ -625,30 +668,47 @@ int cache_es(int dtype) {
   return dtype == KRAKEN_DTYPE_E4M3 ? 1 : dtype == KRAKEN_DTYPE_F32 ? 4 : 2;
 }
 
-// Waves of a call: at most one per tile, and four per CU of the GPU's 256, one per SIMD, as many
-// as LDS holds.
-constexpr int MAX_WAVES = 1024;
-int waves_of(const kraken_paged_cache* c, int n_heads, int max_len) {
-  const int kt = tile_keys(c->head_dim, cache_es(c->dtype));
-  const int64_t units = (int64_t)c->n_sub * c->n_kv_heads * ((n_heads / c->n_kv_heads + 15) / 16);
-  const double tiles = (double)units * c->num_seqs * ((max_len + (int64_t)kt - 1) / kt);
-  return tiles >= MAX_WAVES ? MAX_WAVES : std::max(1, (int)tiles);
+// How a call is shared out.
+struct Shape {
+  int qh, qblocks, q_bytes, waves, entries;      // entries of desc (0: whole units)
+};
+constexpr int WHOLE_TILES = 4;
+Shape shape_of(const kraken_paged_cache* c, int n_heads, int max_len) {
+  Shape s;
+  const int es = cache_es(c->dtype), kt = tile_keys(c->head_dim, es);
+  const int group = n_heads / c->n_kv_heads;
+  s.qh = std::min(16, group);
+  s.qblocks = (group + 15) / 16;
+  s.q_bytes = 2 * q_slot(s.qh, c->head_dim * std::max(es, 2));
+  // as many waves as LDS holds: 35 KB and the queries each of 160 KB per CU
+  const int most = 256 * std::min(4, 163840 / (36864 + s.q_bytes));
+  const int64_t units = (int64_t)c->n_sub * c->n_kv_heads * s.qblocks * c->num_seqs;
+  const int64_t per = (max_len + (int64_t)kt - 1) / kt;
+  const bool whole = per <= WHOLE_TILES;
+  const double items = (double)units * (whole ? 1 : per);
+  s.waves = items >= most ? most : std::max(1, (int)items);
+  s.entries = whole ? 0 : (int)std::min<int64_t>(units, s.waves);
+  return s;
 }
 
 template <typename S, typename C, int HD>
-hipError_t launch_hd(const PagedAttnParams& p, hipStream_t s) {
-  hipLaunchKernelGGL((paged_attn_kernel<S, C, HD>), dim3((unsigned)p.W), dim3(64), 0, s, p);
+hipError_t launch_hd(const PagedAttnParams& p, const Shape& sh, hipStream_t s) {
+  hipLaunchKernelGGL((paged_attn_kernel<S, C, HD>), dim3((unsigned)p.W), dim3(64),
+                     (unsigned)sh.q_bytes, s, p);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !p.desc) return e;
-  hipLaunchKernelGGL((paged_join_kernel<S, HD>), dim3((unsigned)p.W), dim3(256), 0, s, p);
+  if (e != hipSuccess || p.whole) return e;
+  // (about 2048 blocks: more wait for the rest to start and find nothing to do)
+  const int y = std::max(1, std::min(sh.qh, 2048 / sh.entries));
+  hipLaunchKernelGGL((paged_join_kernel<S, HD>), dim3((unsigned)sh.entries, (unsigned)y),
+                     dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
 template <typename S, typename C>
-hipError_t launch_typed(const PagedAttnParams& p, int hd, hipStream_t s) {
-  if (hd == 32) return launch_hd<S, C, 32>(p, s);
-  if (hd == 64) return launch_hd<S, C, 64>(p, s);
-  return launch_hd<S, C, 128>(p, s);
+hipError_t launch_typed(const PagedAttnParams& p, const Shape& sh, int hd, hipStream_t s) {
+  if (hd == 32) return launch_hd<S, C, 32>(p, sh, s);
+  if (hd == 64) return launch_hd<S, C, 64>(p, sh, s);
+  return launch_hd<S, C, 128>(p, sh, s);
 }
 
 kraken_status fail(kraken_status s, const char* msg) { return (kraken_status)set_error(s, msg); }
@@ -667,11 +727,9 @@ int64_t kraken_paged_attention_work_floats(const kraken_paged_cache* cache, int3
       n_heads % cache->n_kv_heads != 0 || max_len < 0 ||
       max_len > (int64_t)cache->pages_per_seq * cache->page_size)
     return -1;
-  // a unit of one tile is never split
-  if (max_len <= tile_keys(cache->head_dim, cache_es(cache->dtype))) return 0;
-  const int64_t W = waves_of(cache, n_heads, max_len);
-  const int64_t qh = std::min(16, n_heads / cache->n_kv_heads);
-  return W * (4 + 2 * qh * (2 + cache->head_dim));
+  const Shape sh = shape_of(cache, n_heads, max_len);
+  if (sh.entries == 0) return 0;
+  return 4 * (int64_t)sh.entries + 2 * (int64_t)sh.waves * sh.qh * (2 + cache->head_dim);
 }
 
 kraken_status kraken_op_paged_attention(int32_t dtype, const kraken_rows* q,
@@ -711,23 +769,27 @@ kraken_status kraken_op_paged_attention(int32_t dtype, const kraken_rows* q,
   p.out = {out->data, out->sub_stride, out->row_stride};
   p.lens = lens; p.fault = fault;
   p.heads = n_heads; p.group = n_heads / cache->n_kv_heads; p.max_len = max_len;
-  p.qblocks = (p.group + 15) / 16;
-  p.qh = std::min(16, p.group);
-  p.W = waves_of(cache, n_heads, max_len);
+  const Shape sh = shape_of(cache, n_heads, max_len);
+  p.qblocks = sh.qblocks;
+  p.qh = sh.qh;
+  p.W = sh.waves;
+  p.whole = sh.entries == 0;
+  p.by_unit = 0;
   p.desc = nullptr;
   p.ml = p.o = nullptr;
-  if (need > 0) {
+  if (!p.whole) {
+    p.by_unit = (int64_t)cache->n_sub * cache->n_kv_heads * sh.qblocks * cache->num_seqs <= p.W;
     p.desc = reinterpret_cast<int4*>(work);
-    p.ml = work + 4 * (int64_t)p.W;
+    p.ml = work + 4 * (int64_t)sh.entries;
     p.o = p.ml + 4 * (int64_t)p.W * p.qh;
   }
   p.scale = scale != 0.f ? scale : (float)(1.0 / sqrt((double)hd));
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e;
-  if (dtype == KRAKEN_DTYPE_F32) e = launch_typed<float, float>(p, hd, s);
+  if (dtype == KRAKEN_DTYPE_F32) e = launch_typed<float, float>(p, sh, hd, s);
   else if (dtype == KRAKEN_DTYPE_BF16)
-    e = e4m3_cache ? launch_typed<bf16, e4m3>(p, hd, s) : launch_typed<bf16, bf16>(p, hd, s);
-  else e = e4m3_cache ? launch_typed<f16, e4m3>(p, hd, s) : launch_typed<f16, f16>(p, hd, s);
+    e = e4m3_cache ? launch_typed<bf16, e4m3>(p, sh, hd, s) : launch_typed<bf16, bf16>(p, sh, hd, s);
+  else e = e4m3_cache ? launch_typed<f16, e4m3>(p, sh, hd, s) : launch_typed<f16, f16>(p, sh, hd, s);
   if (e == hipSuccess) return KRAKEN_OK;
   return fail(KRAKEN_ERR_HIP, hipGetErrorString(e));
 }
