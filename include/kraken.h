@@ -582,14 +582,15 @@ kraken_status kraken_op_paged_append(int32_t dtype, const kraken_rows* q, const 
  *   out      rows of n_heads * head_dim elements of `dtype`, not overlapping the inputs
  *   lens     device int32 [num_seqs]: tokens that sequence b attends to, the new token's own,
  *            which the append has written, among them.  0: a padding row, its output is zeros.
- *   max_len  HOST: no lens[b] exceeds it, 0 .. pages_per_seq * page_size, with num_seqs *
- *            max_len below 2^35.  The launch is sized
+ *   max_len  HOST: no lens[b] exceeds it, 0 .. pages_per_seq * page_size.  The launch is sized
  *            by it: the tighter it is, the better.
  *   scale    factor of the scores; 0 means 1 / sqrt(head_dim)
  *   cache    dtype equal to `dtype`, or E4M3 with `dtype` BF16 or F16
  *   work     device float32 scratch, 16-byte aligned, of work_floats >=
  *            kraken_paged_attention_work_floats(cache, n_heads, max_len); NULL if that is 0.
  *            It need not hold anything; calls that may run at one time need one each.
+ * Sizes: the keys of all heads and sequences, if every one had max_len, fill fewer than 2^31
+ * tiles (8 KB of one head's keys, at most 128 keys).
  * Scores, softmax and sums are fp32.  Positions at or past lens[b] are never read.  The same
  * call gives the same bits.  A row whose length is out of range (0 .. max_len) or that needs a
  * page out of range gives NaN and sets *fault.  Errors: INVALID_ARG, UNSUPPORTED, HIP.

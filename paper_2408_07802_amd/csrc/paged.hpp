@@ -53,11 +53,11 @@ KRAKEN_HD int64_t paged_row(const PagedView& c, int i, int kv, int page, int h) 
   return ((((int64_t)i * 2 + kv) * c.pages + page) * c.heads + h) * (int64_t)c.page.d;
 }
 
-// A list of `total` items in `runs` (1 .. total) equal runs: the first item of run w, and the
-// last run that holds an item at or before `item` of its own.
-KRAKEN_HD int64_t split_begin(int64_t total, int runs, int w) { return total * w / runs; }
-KRAKEN_HD int split_last(int64_t total, int runs, int64_t item) {
-  return (int)(((item + 1) * runs - 1) / total);
+// Items of each run where a list of total >= 0 (below 2^31) items is cut into at most runs.d
+// equal ones (the last may be shorter): item x lies in run x / that.
+KRAKEN_HD int run_length(FastDiv runs, int total) {
+  const int q = (int)div_of(runs, (uint32_t)total);
+  return q + ((uint32_t)q * runs.d < (uint32_t)total || q == 0 ? 1 : 0);
 }
 
 // Checks a cache's description (with_data: its pointers, too) and fills view; a message and

@@ -23,6 +23,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "kraken_internal.hpp"
 #include "paged.hpp"
@@ -44,6 +45,7 @@ struct PagedAttnParams {
   float* ml;            // [W][2][qh][2]: maximum and sum
   float* o;             // [W][2][qh][HD]: unnormalised output
   int heads, group, max_len, W;
+  FastDiv per_run, per_seq, per_block, per_head;   // by W, units of a sequence, qblocks, kv heads
   int qblocks, qh;      // blocks of query heads per key/value head; query heads per block (<= 16)
   int whole;            // runs end where units end: nothing is shared
   int by_unit;          // desc has an entry per unit (of every sequence), not per run
@@ -53,6 +55,7 @@ struct PagedAttnParams {
 typedef uint8_t e4m3;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) void* lds_ptr;
@@ -61,15 +64,20 @@ __device__ __forceinline__ uint32_t lds_addr(const void* p) {
   return (uint32_t)(uintptr_t)(lds_ptr)p;
 }
 
-// 16 (4) bytes per lane from global memory into LDS at `lds` + 16 (4) * lane.  Counted by
-// vmcnt, which the kernel waits for itself.
-__device__ __forceinline__ void dma16(uint32_t lds, const void* g) {
+// 16 (4) bytes per lane from global memory into LDS at `lds` + 16 (4) * lane; lds is uniform.
+// Counted by vmcnt, which the kernel waits for itself.
+__device__ __forceinline__ void dma16(uint32_t lds, uint64_t g) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-               :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(g) : "memory", "m0");
+               :: "s"(lds), "v"(g) : "memory", "m0");
 }
 __device__ __forceinline__ void dma4(uint32_t lds, const void* g) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
-               :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(g) : "memory", "m0");
+               :: "s"(lds), "v"(g) : "memory", "m0");
+}
+// What lies at an LDS address.
+template <typename V>
+__device__ __forceinline__ V lds_read(uint32_t at) {
+  return *(const __attribute__((address_space(3))) V*)at;
 }
 // Waits until at most N of the wave's vector memory operations are outstanding (they complete
 // in order).
@@ -80,6 +88,30 @@ __device__ __forceinline__ void wait_vm() {
 }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// x of lane ^ 16 (^ 32) and the lane's own, in an order that both lanes share.
+struct Both {
+  float a, b;
+};
+template <bool BY32>
+__device__ __forceinline__ Both with_other(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto r = BY32 ? __builtin_amdgcn_permlane32_swap(u, u, false, false)
+                      : __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t a = r[0], b = r[1];
+  return {__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
+}
+// Of the four lanes lane % 16 + 16 k: the maximum, and the sum.
+__device__ __forceinline__ float max4(float x) {
+  const Both p = with_other<false>(x);
+  const Both q = with_other<true>(fmaxf(p.a, p.b));
+  return fmaxf(q.a, q.b);
+}
+__device__ __forceinline__ float sum4(float x) {
+  const Both p = with_other<false>(x);
+  const Both q = with_other<true>(p.a + p.b);
+  return q.a + q.b;
+}
 
 // Sizes of a tile.  C: the cache's element type.
 template <typename C, int HD>
@@ -156,17 +188,18 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
   using T = Tile<C, HD>;
   constexpr bool F32 = sizeof(C) == 4, F8 = sizeof(C) == 1;
   constexpr int KT = T::KT, KB = KT / 16, FT = HD / 16, NT = T::NT, ND = 2 * T::NI;
-  __shared__ __align__(1024) uint8_t kv[2][2][KT * T::RB];     // [stage][K, V]
+  constexpr int RBQ = HD * (int)sizeof(S), STAGE = KT * T::RB;
+  __shared__ __align__(1024) uint8_t kv[2][2][STAGE];          // [stage][K, V]
   __shared__ int pg[4][NT * 64];                               // pages of a tile's rows
+  __shared__ uint64_t row_at[NT * 64];                         // and where its K rows lie
   __shared__ int s_len[KRAKEN_MAX_SEQS];                       // keys, -1: out of range
   extern __shared__ __align__(16) uint8_t q_rows[];            // [2][q_slot]
 
   const int lane = threadIdx.x, w = blockIdx.x, g = lane >> 4, col = lane & 15;
-  const int B = p.cache.seqs, U = p.cache.n * p.cache.heads * p.qblocks;
+  const int B = p.cache.seqs, U = (int)p.per_seq.d;
 
   // lengths, and the tiles of sequences 0 .. b for the lane's four
-  int64_t total;
-  int incl[4];
+  int total, incl[4];
   {
     int sum = 0;
 #pragma unroll
@@ -186,13 +219,13 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) incl[e] += scan - sum;
-    total = (int64_t)uniform(__shfl(scan, 63, 64)) * U;
+    total = uniform(__shfl(scan, 63, 64)) * U;
   }
   auto len_of = [&](int b) { return uniform(s_len[b]); };
 
   // rows without keys: zeros, or NaN for a length out of range
   for (int r = w; r < p.cache.n * B; r += gridDim.x) {
-    const int i = r / B, b = r % B, len = len_of(b);
+    const int i = r / B, b = r - i * B, len = len_of(b);
     if (len > 0) continue;
     if (p.by_unit)
       for (int u = lane; u < p.cache.heads * p.qblocks; u += 64)
@@ -201,15 +234,12 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
     S* out = static_cast<S*>(p.out.data) + i * p.out.sub + b * p.out.row;
     for (int c = lane; c < p.heads * HD; c += 64) out[c] = len < 0 ? (S)NAN : (S)0.f;
   }
-
-  const int W = (int)(total < p.W ? total : p.W);              // waves with work
   if (p.desc && !p.by_unit && lane == 0) p.desc[w] = make_int4(0, 0, 0, 0);
-  if (w >= W) return;
 
   // sequence, unit and tile of an item of the list
-  auto place_of = [&](int64_t item) {
+  auto place_of = [&](int item) {
     Place c;
-    const int x = (int)(item / U);
+    const int x = (int)div_of(p.per_seq, (uint32_t)item);
     int b = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) b += __popcll(__ballot(incl[e] <= x));
@@ -219,25 +249,16 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
     c.nt = (c.len + KT - 1) / KT;
     // tiles before b: its own inclusive count less its tiles
     const int own = (b & 3) == 0 ? incl[0] : (b & 3) == 1 ? incl[1] : (b & 3) == 2 ? incl[2] : incl[3];
-    const int64_t rem = item - (int64_t)(uniform(__shfl(own, b >> 2, 64)) - c.nt) * U;
-    c.u = (int)(rem / c.nt);
-    c.j = (int)(rem - (int64_t)c.u * c.nt);
-    c.qb = c.u % p.qblocks;
-    c.h = c.u / p.qblocks % p.cache.heads;
-    c.i = c.u / p.qblocks / p.cache.heads;
+    const uint32_t rem = (uint32_t)(item - (uniform(__shfl(own, b >> 2, 64)) - c.nt) * U);
+    c.u = uniform((int)(rem / (uint32_t)c.nt));
+    c.j = (int)rem - c.u * c.nt;
+    const int hq = (int)div_of(p.per_block, (uint32_t)c.u);
+    c.qb = c.u - hq * p.qblocks;
+    c.i = (int)div_of(p.per_head, (uint32_t)hq);
+    c.h = hq - c.i * p.cache.heads;
     c.bad = 0;
     return c;
   };
-  // an item, or the first behind its unit where it lies inside one and units are not shared
-  auto edge = [&](int64_t item) {
-    if (!p.whole || item == 0 || item == total) return item;
-    const Place c = place_of(item);
-    return c.j == 0 ? item : item + c.nt - c.j;
-  };
-  const int64_t begin = edge(split_begin(total, W, w));
-  const int cnt = (int)(edge(split_begin(total, W, w + 1)) - begin);
-  if (cnt == 0) return;
-  Place tp = place_of(begin);                                  // of the next tile to look up
   auto advance = [&](Place& c) {
     if (++c.j < c.nt) return;
     c.j = 0;
@@ -253,8 +274,41 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
     c.nt = (c.len + KT - 1) / KT;
   };
 
-  const int64_t page_bytes = (int64_t)p.cache.heads * p.cache.page.d * T::RB;
-  const int64_t v_off = p.cache.pages * page_bytes;
+  // the run: items begin .. begin + cnt - 1, and the place of the next tile to look up.  Where
+  // units are not shared, an edge inside a unit moves behind it.
+  const int run = run_length(p.per_run, total);
+  int begin = w * run;
+  if (begin >= total) return;
+  int end = min(begin + run, total);
+  Place tp = place_of(begin);
+  if (p.whole) {
+    if (end < total) {
+      const Place e = place_of(end);
+      if (e.j > 0) end += e.nt - e.j;
+    }
+    if (tp.j > 0) {
+      begin += tp.nt - tp.j;
+      tp.j = tp.nt - 1;
+      if (begin < end) advance(tp);
+    }
+  }
+  const int cnt = end - begin;
+  if (cnt <= 0) return;
+
+  const uint32_t page_bytes = (uint32_t)p.cache.heads * p.cache.page.d * T::RB;
+  const uint64_t v_off = (uint64_t)p.cache.pages * page_bytes;
+  const uint32_t kv_at = lds_addr(kv), q_at = lds_addr(q_rows);
+  const uint32_t q_step = q_slot(p.qh, RBQ);
+  // this lane's chunk of a DMA instruction's K and V rows: bytes behind the row's beginning
+  uint32_t k_off[T::NI];
+  uint64_t v_at[T::NI];
+#pragma unroll
+  for (int x = 0; x < T::NI; ++x) {
+    const int r = x * T::RPI + lane / T::NC, pc = lane % T::NC;
+    k_off[x] = (pc ^ k_key<C, HD>(r)) * 16;
+    v_at[x] = v_off + (pc ^ v_key<C, HD>(r)) * 16;
+  }
+
   // page numbers of a tile's rows; rows behind the last key are the last key's
   auto look_up = [&](const Place& c, int slot) {
     const int32_t* row = p.cache.table + (int64_t)c.b * p.cache.table_ld;
@@ -265,35 +319,37 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
     }
   };
   // a tile's rows, behind the queries of a unit that begins with it
-  constexpr int RBQ = HD * (int)sizeof(S);
   auto fetch = [&](Place& c, int slot, int stage, bool first) {
-    if (c.j == 0 || first) {             // a unit's queries, adjacent rows
-      const int qb16 = c.qb * 16, nh = min(16, p.group - qb16);
-      const uint8_t* src = reinterpret_cast<const uint8_t*>(
+    if (c.j == 0 || first) {
+      const int nh = min(16, p.group - c.qb * 16);
+      const uint64_t src = reinterpret_cast<uint64_t>(
           static_cast<const S*>(p.q.data) + c.i * p.q.sub + c.b * p.q.row +
-          (int64_t)(c.h * p.group + qb16) * HD);
-      const uint32_t to = lds_addr(q_rows) + stage * q_slot(p.qh, RBQ);
+          (int64_t)(c.h * p.group + c.qb * 16) * HD);
       for (int x = 0; x < nh * RBQ; x += 1024)
-        dma16(to + x, src + min(x + lane * 16, nh * RBQ - 16));
+        dma16(uniform((int)(q_at + stage * q_step + x)), src + min(x + lane * 16, nh * RBQ - 16));
     }
-    const uint8_t* base = static_cast<const uint8_t*>(p.cache.data) +
-                          2 * c.i * v_off + (int64_t)c.h * p.cache.page.d * T::RB;
+    const uint64_t base = reinterpret_cast<uint64_t>(p.cache.data) + 2 * c.i * v_off +
+                          (uint64_t)((uint32_t)c.h * p.cache.page.d * T::RB);
     bool bad = false;
 #pragma unroll
-    for (int x = 0; x < T::NI; ++x) {
-      const int r = x * T::RPI + lane / T::NC, key = min(c.j * KT + r, c.len - 1);
-      const int place = key - (int)(div_of(p.cache.page, (uint32_t)key) * p.cache.page.d);
-      int page = pg[slot][r];
+    for (int x = 0; x < NT; ++x) {
+      const int key = min(c.j * KT + x * 64 + lane, c.len - 1);
+      const uint32_t at = ((uint32_t)key - div_of(p.cache.page, (uint32_t)key) * p.cache.page.d) *
+                          (uint32_t)T::RB;
+      int page = pg[slot][x * 64 + lane];
       const bool ok = page >= 0 && page < p.cache.pages;
       bad |= !ok;
       page = ok ? page : 0;
-      const uint8_t* at = base + (uint64_t)(uint32_t)page * (uint32_t)page_bytes +
-                          (uint32_t)(place * T::RB);
-      const int pc = lane % T::NC;
-      dma16(lds_addr(&kv[stage][0][x * 1024]), at + (pc ^ k_key<C, HD>(r)) * 16);
-      dma16(lds_addr(&kv[stage][1][x * 1024]), at + v_off + (pc ^ v_key<C, HD>(r)) * 16);
+      row_at[x * 64 + lane] = base + (uint64_t)(uint32_t)page * page_bytes + at;
     }
     c.bad = __any(bad);
+    const uint32_t to = kv_at + stage * (2 * STAGE);
+#pragma unroll
+    for (int x = 0; x < T::NI; ++x) {
+      const uint64_t at = row_at[x * T::RPI + lane / T::NC];
+      dma16(to + x * 1024, at + k_off[x]);
+      dma16(to + STAGE + x * 1024, at + v_at[x]);
+    }
   };
 
   // state of the unit at hand: the lane's query head col
@@ -307,13 +363,12 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
   auto open_unit = [&](const Place& c, int stage) {
     h0 = c.h * p.group + c.qb * 16;
     nh = min(16, p.group - c.qb * 16);
-    const S* src = reinterpret_cast<const S*>(q_rows + stage * q_slot(p.qh, RBQ)) +
-                   min(col, nh - 1) * HD;
+    const uint32_t src = q_at + stage * q_step + min(col, nh - 1) * RBQ;
     const bool mine = col < nh;
     if constexpr (F32) {
 #pragma unroll
       for (int m = 0; m < HD / 16; ++m) {
-        q4[m] = *reinterpret_cast<const f32x4*>(src + 16 * m + 4 * g);
+        q4[m] = lds_read<f32x4>(src + (16 * m + 4 * g) * 4);
         if (!mine) q4[m] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
     } else {
@@ -321,8 +376,8 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
       for (int m = 0; m < HD / 32; ++m) {
         // dimensions of k slot 8 g + e of product m: as the K operand's
         const int at = F8 && HD > 32 ? 64 * (m / 2) + 16 * g + 8 * (m % 2) : 32 * m + 8 * g;
-        uint4 v = *reinterpret_cast<const uint4*>(src + at);
-        if (!mine) v = make_uint4(0, 0, 0, 0);
+        i32x4 v = lds_read<i32x4>(src + at * 2);
+        if (!mine) v = i32x4{0, 0, 0, 0};
         q[m] = __builtin_bit_cast(Vec8<S>, v);
       }
     }
@@ -340,95 +395,112 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
     for (int f = 0; f < FT; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
   };
 
+  // This lane's LDS addresses, all but constants: chunk (4 m + g) ^ key of K row col (the key of
+  // rows col + 16 kb is the same), and its part of V rows.  (Chunks are permuted within the
+  // aligned bytes of a row, so the permuted chunk of block f is one exclusive or away.)
+  const uint32_t k_row = kv_at + col * T::RB;
+  const int k_k = k_key<C, HD>(col);
   auto compute = [&](const Place& c, int stage) {
-    const uint8_t* K = kv[stage][0];
-    const uint8_t* V = kv[stage][1];
+    const uint32_t K = k_row + stage * (2 * STAGE);
     f32x4 sc[KB];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      const int r = kb * 16 + col;
-      const uint8_t* row = K + r * T::RB;
-      const int key = k_key<C, HD>(r);
-      sc[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if constexpr (F32) {
+    for (int kb = 0; kb < KB; ++kb) sc[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (F32) {
 #pragma unroll
-        for (int m = 0; m < HD / 16; ++m) {
-          const f32x4 a = *reinterpret_cast<const f32x4*>(row + ((4 * m + g) ^ key) * 16);
+      for (int m = 0; m < HD / 16; ++m) {
+        const uint32_t at = K + ((4 * m + g) ^ k_k) * 16;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const f32x4 a = lds_read<f32x4>(at + kb * 16 * T::RB);
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             sc[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], q4[m][e], sc[kb], 0, 0, 0);
         }
-      } else if constexpr (F8 && HD == 32) {
-        const uint2 a = *reinterpret_cast<const uint2*>(row + ((g / 2) ^ key) * 16 + g % 2 * 8);
-        sc[kb] = mfma32<S>(from_e4m3<S>(a.x, a.y), q[0], sc[kb]);
-      } else if constexpr (F8) {
+      }
+    } else if constexpr (F8 && HD == 32) {
+      const uint32_t at = K + ((g / 2) ^ k_k) * 16 + g % 2 * 8;
 #pragma unroll
-        for (int m = 0; m < HD / 64; ++m) {
-          const uint4 a = *reinterpret_cast<const uint4*>(row + ((4 * m + g) ^ key) * 16);
-          sc[kb] = mfma32<S>(from_e4m3<S>(a.x, a.y), q[2 * m], sc[kb]);
-          sc[kb] = mfma32<S>(from_e4m3<S>(a.z, a.w), q[2 * m + 1], sc[kb]);
-        }
-      } else {
+      for (int kb = 0; kb < KB; ++kb) {
+        const i32x2 a = lds_read<i32x2>(at + kb * 16 * T::RB);
+        sc[kb] = mfma32<S>(from_e4m3<S>(a[0], a[1]), q[0], sc[kb]);
+      }
+    } else if constexpr (F8) {
 #pragma unroll
-        for (int m = 0; m < HD / 32; ++m) {
-          const uint4 a = *reinterpret_cast<const uint4*>(row + ((4 * m + g) ^ key) * 16);
-          sc[kb] = mfma32<S>(__builtin_bit_cast(Vec8<S>, a), q[m], sc[kb]);
+      for (int m = 0; m < HD / 64; ++m) {
+        const uint32_t at = K + ((4 * m + g) ^ k_k) * 16;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const i32x4 a = lds_read<i32x4>(at + kb * 16 * T::RB);
+          sc[kb] = mfma32<S>(from_e4m3<S>(a[0], a[1]), q[2 * m], sc[kb]);
+          sc[kb] = mfma32<S>(from_e4m3<S>(a[2], a[3]), q[2 * m + 1], sc[kb]);
         }
+      }
+    } else {
+#pragma unroll
+      for (int m = 0; m < HD / 32; ++m) {
+        const uint32_t at = K + ((4 * m + g) ^ k_k) * 16;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+          sc[kb] = mfma32<S>(lds_read<Vec8<S>>(at + kb * 16 * T::RB), q[m], sc[kb]);
       }
     }
     // scores in base-2 units, of keys 16 kb + 4 g + r
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) sc[kb] *= ks;
     const int left = c.len - c.j * KT;
+    if (left < KT) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (kb * 16 + 4 * g + r >= left) sc[kb][r] = -INFINITY;
+    }
     float mx = -INFINITY;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float s = sc[kb][r] * ks;
-        if (left < KT && kb * 16 + 4 * g + r >= left) s = -INFINITY;
-        sc[kb][r] = s;
-        mx = fmaxf(mx, s);
-      }
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      mx = fmaxf(mx, fmaxf(fmaxf(sc[kb][0], sc[kb][1]), fmaxf(sc[kb][2], sc[kb][3])));
+    mx = max4(mx);
     if (__any(mx > m_run)) {
       const float m_new = fmaxf(m_run, mx);
       // (a head without a finite score yet has sums of zero, which any factor but NaN keeps)
       const float alpha = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
       l_run *= alpha;
 #pragma unroll
-      for (int f = 0; f < FT; ++f)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[f][r] *= alpha;
+      for (int f = 0; f < FT; ++f) acc[f] *= alpha;
       m_run = m_new;
     }
     const float mref = m_run == -INFINITY ? 0.f : m_run;
-    float ps = 0.f;
+    f32x4 ps = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
+    for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        sc[kb][r] = __builtin_amdgcn_exp2f(sc[kb][r] - mref);
-        ps += sc[kb][r];
-      }
-    l_run += ps;                              // of the lane's keys; the lanes join at the end
+      for (int r = 0; r < 4; ++r) sc[kb][r] = __builtin_amdgcn_exp2f(sc[kb][r] - mref);
+      ps += sc[kb];
+    }
+    // of the lane's keys; the lanes join at the end
+    l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+    const uint32_t V = kv_at + stage * (2 * STAGE) + STAGE;
     if constexpr (F32) {
       constexpr int E = HD < 64 ? 2 : 4;      // features 16 E cc + E row + e of one LDS read
+      const uint32_t at = V + 4 * g * T::RB + col * 4 * E;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const uint8_t* row = V + (kb * 16 + 4 * g + r) * T::RB;
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
           for (int cc = 0; cc < FT / E; ++cc) {
             typedef float vec __attribute__((ext_vector_type(E)));
-            const vec v = *reinterpret_cast<const vec*>(row + (cc * 16 + col) * 4 * E);
+            const vec v = lds_read<vec>(at + (kb * 16 + r) * T::RB + cc * 64 * E);
 #pragma unroll
             for (int e = 0; e < E; ++e)
               acc[cc * E + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], sc[kb][r],
                                                                      acc[cc * E + e], 0, 0, 0);
           }
-        }
     } else {
+      // the lane's row of block f's reads: 8 bits, of 8 rows; 16 bits, of 4 (and 16 further on)
+      const int e = col / 2, r0 = F8 ? 16 * (e / 4) + 4 * g + e % 4 : 4 * g + col / 4;
+      const uint32_t at = V + r0 * T::RB + (col & 1) * 8 +
+                          ((F8 ? 0 : (col & 3) / 2) ^ v_key<C, HD>(r0)) * 16;
 #pragma unroll
       for (int k2 = 0; k2 < KB / 2; ++k2) {
         // k slots 8 g + e: keys 4 g + e of block 2 k2, then of the next.  A weight goes into
@@ -436,30 +508,25 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
         // keeps 16 bits of it and more, and the second product is free next to the loads.
         Vec8<S> hi, lo;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float x = sc[2 * k2 + e / 4][e % 4];
-          hi[e] = (S)x;
-          lo[e] = (S)(x - (float)hi[e]);
+        for (int x = 0; x < 8; ++x) {
+          const float v = sc[2 * k2 + x / 4][x % 4];
+          hi[x] = (S)v;
+          lo[x] = (S)(v - (float)hi[x]);
         }
 #pragma unroll
         for (int f = 0; f < FT; ++f) {
           Vec8<S> a;
           if constexpr (F8) {
-            const int e = col / 2, r = k2 * 32 + 16 * (e / 4) + 4 * g + e % 4;
             const i32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                (__attribute__((address_space(3))) i32x2*)(
-                    V + r * T::RB + (f ^ v_key<C, HD>(r)) * 16 + (col & 1) * 8));
+                (__attribute__((address_space(3))) i32x2*)((at ^ (f * 16)) + k2 * 32 * T::RB));
             a = from_e4m3<S>((uint32_t)x[0], (uint32_t)x[1]);
           } else {
             s16x4 x[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int r = k2 * 32 + 16 * e + 4 * g + col / 4;
-              x[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  (__attribute__((address_space(3))) s16x4*)(
-                      V + r * T::RB + ((2 * f + (col & 3) / 2) ^ v_key<C, HD>(r)) * 16 +
-                      (col & 1) * 8));
-            }
+            for (int y = 0; y < 2; ++y)
+              x[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                  (__attribute__((address_space(3))) s16x4*)((at ^ (f * 32)) +
+                                                             (k2 * 32 + y * 16) * T::RB));
             typedef short s16x8 __attribute__((ext_vector_type(8)));
             const s16x8 both = __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
             a = __builtin_bit_cast(Vec8<S>, both);
@@ -489,11 +556,9 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
   };
 
   // end of the unit (done) or of the wave's run in the middle of it
-  auto close_unit = [&](const Place& c, int64_t at) {
+  auto close_unit = [&](const Place& c, int at) {
     const bool done = c.j == c.nt - 1;
-    float l = l_run;
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
+    float l = sum4(l_run);
     if (bad) {
       l = NAN;
       if (p.fault && lane == 0) *p.fault = 1;
@@ -519,7 +584,7 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
     }
     const int slot = 2 * w + (began ? 1 : 0);
     if (began && lane == 0) {
-      const int last = split_last(total, W, at + (c.nt - 1 - c.j));
+      const int last = (int)((uint32_t)(at + c.nt - 1 - c.j) / (uint32_t)run);
       p.desc[p.by_unit ? c.b * U + c.u : w] = make_int4(last - w + 1, w, c.b, c.u);
     }
     if (col < nh) {
@@ -671,6 +736,7 @@ int cache_es(int dtype) {
 // How a call is shared out.
 struct Shape {
   int qh, qblocks, q_bytes, waves, entries;      // entries of desc (0: whole units)
+  double tiles;                                  // at most
 };
 constexpr int WHOLE_TILES = 4;
 Shape shape_of(const kraken_paged_cache* c, int n_heads, int max_len) {
@@ -680,11 +746,12 @@ Shape shape_of(const kraken_paged_cache* c, int n_heads, int max_len) {
   s.qh = std::min(16, group);
   s.qblocks = (group + 15) / 16;
   s.q_bytes = 2 * q_slot(s.qh, c->head_dim * std::max(es, 2));
-  // as many waves as LDS holds: 35 KB and the queries each of 160 KB per CU
-  const int most = 256 * std::min(4, 163840 / (36864 + s.q_bytes));
+  // as many waves as LDS holds: 37 KB and the queries each of 160 KB per CU
+  const int most = 256 * std::min(4, 163840 / (37888 + s.q_bytes));
   const int64_t units = (int64_t)c->n_sub * c->n_kv_heads * s.qblocks * c->num_seqs;
   const int64_t per = (max_len + (int64_t)kt - 1) / kt;
   const bool whole = per <= WHOLE_TILES;
+  s.tiles = (double)units * per;
   const double items = (double)units * (whole ? 1 : per);
   s.waves = items >= most ? most : std::max(1, (int)items);
   s.entries = whole ? 0 : (int)std::min<int64_t>(units, s.waves);
@@ -751,8 +818,6 @@ kraken_status kraken_op_paged_attention(int32_t dtype, const kraken_rows* q,
     return fail(KRAKEN_ERR_INVALID_ARG, "n_kv_heads does not divide n_heads");
   if (max_len < 0 || max_len > (int64_t)cache->pages_per_seq * cache->page_size)
     return fail(KRAKEN_ERR_INVALID_ARG, "max_len out of 0..pages_per_seq * page_size");
-  if ((int64_t)cache->num_seqs * max_len >= (1ll << 35))
-    return fail(KRAKEN_ERR_UNSUPPORTED, "num_seqs * max_len must stay below 2^35");
   if (!isfinite(scale)) return fail(KRAKEN_ERR_INVALID_ARG, "scale is not finite");
   const int es = dtype == KRAKEN_DTYPE_F32 ? 4 : 2;
   for (const kraken_rows* r : {q, out})
@@ -770,7 +835,13 @@ kraken_status kraken_op_paged_attention(int32_t dtype, const kraken_rows* q,
   p.lens = lens; p.fault = fault;
   p.heads = n_heads; p.group = n_heads / cache->n_kv_heads; p.max_len = max_len;
   const Shape sh = shape_of(cache, n_heads, max_len);
+  if (sh.tiles >= 2147483648.0)
+    return fail(KRAKEN_ERR_UNSUPPORTED, "2^31 or more tiles of keys");
   p.qblocks = sh.qblocks;
+  p.per_run = fast_div((uint32_t)sh.waves);
+  p.per_seq = fast_div((uint32_t)(cache->n_sub * cache->n_kv_heads * sh.qblocks));
+  p.per_block = fast_div((uint32_t)sh.qblocks);
+  p.per_head = fast_div((uint32_t)cache->n_kv_heads);
   p.qh = sh.qh;
   p.W = sh.waves;
   p.whole = sh.entries == 0;

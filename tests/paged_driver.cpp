@@ -58,23 +58,14 @@ int main() {
       }
   }
 
-  // runs: every item in one run, run lengths that differ by at most one, and the last run of
-  // an item
-  for (int k = 0; k < 3000; ++k) {
-    const int64_t total = 1 + (int64_t)(rng() % (k % 2 ? 5000 : 60));
-    const int runs = (int)(1 + rng() % (total < 1024 ? total : 1024));
-    CHECK(split_begin(total, runs, 0) == 0 && split_begin(total, runs, runs) == total);
-    for (int w = 0; w < runs; ++w) {
-      const int64_t a = split_begin(total, runs, w), e = split_begin(total, runs, w + 1);
-      CHECK(e - a >= total / runs && e - a <= (total + runs - 1) / runs && e > a);
-      for (int64_t item = a; item < e; ++item) CHECK(split_last(total, runs, item) == w);
-    }
-  }
-  // (a list as long as a call can have: 2^31 tiles of 2^24 units)
-  const int64_t big = (1ll << 31) * (1ll << 21);
-  for (int w = 0; w < 1024; ++w) {
-    const int64_t a = split_begin(big, 1024, w);
-    CHECK(split_last(big, 1024, a) == w && (w == 0 || split_last(big, 1024, a - 1) == w - 1));
+  // runs: no more than asked for, every item in the run of its quotient, and no run longer
+  // than an even share rounded up
+  for (int k = 0; k < 20000; ++k) {
+    const int total = k % 3 ? (int)(rng() % 5000) : (int)(rng() >> 33);
+    const int runs = (int)(1 + rng() % 1024);
+    const int len = run_length(fast_div((uint32_t)runs), total);
+    CHECK(len >= 1 && len == (total == 0 ? 1 : (total + (int64_t)runs - 1) / runs));
+    CHECK(((int64_t)total + len - 1) / len <= runs);
   }
   std::puts("paged index arithmetic holds");
   return 0;
