@@ -44,9 +44,12 @@ COMMON_FLAGS = [
 
 # Per-file additions.  Attention: for finite inputs its softmax only takes maxima of finite
 # scores and -inf; without IEEE mode the compiler drops the NaN-quieting instruction it
-# otherwise puts in front of every maximum.
+# otherwise puts in front of every maximum.  Paged attention: its accumulators are rescaled by
+# vector instructions, so the matrix products keep them in vector registers (in accumulation
+# registers, every rescaling moved them there and back: 1600 moves in the file's kernels).
 FILE_FLAGS = {
     "attention.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"],
+    "paged_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 
 
