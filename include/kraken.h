@@ -497,7 +497,7 @@ kraken_status kraken_op_decode_attention_noalloc(int32_t dtype, const void* qk,
  *           table[b][p / page_size], place p % page_size.  Sequences may share pages that
  *           nothing appends to.  Entries that no position below needs are never read.
  *   scales  dtype E4M3: device float32 [n_sub][2][n_kv_heads]; an element stands for
- *           scale * its value.  NULL for the other types.
+ *           scale * its value.  Positive, 2^-126 or more.  NULL for the other types.
  *   num_seqs       rows of the table, 1 .. KRAKEN_MAX_SEQS
  *   pages_per_seq  entries of a row (a sequence's capacity is pages_per_seq * page_size, below
  *                  2^31); table_ld >= pages_per_seq

@@ -7,6 +7,7 @@
 // whole turns are dropped there, and only the rest in [-1/2, 1/2] goes to fp32.
 #include <hip/hip_runtime.h>
 #include <math.h>
+#include <algorithm>
 
 #include "kraken_internal.hpp"
 #include "paged.hpp"
@@ -21,13 +22,22 @@ struct RowsView {
   int64_t sub, row;                   // elements between sub-layers and between rows
 };
 
+// The rows of one kind (queries, keys or values): where they come from, where they go as rows
+// (data NULL: nowhere), and how blocks share them.
+struct Part {
+  RowsView in, out;
+  int units, rows;                    // units of a row; rows of a block
+  FastDiv per_row;                    // by units
+  unsigned first;                     // block
+};
+
 struct AppendParams {
-  RowsView q, k, v, q_out, k_out;     // (data NULL: absent)
+  Part part[3];                       // 0: queries (in.data NULL: none), 1: keys, 2: values
   PagedView cache;
   const int32_t* pos;
   const int32_t* seq;
   int32_t* fault;
-  int T, heads, hd, rot, neighbours;
+  int T, hd, rot, neighbours;
   double turns[MAX_FREQ];             // inv_freq / (2 pi)
 };
 
@@ -36,20 +46,7 @@ struct alignas(sizeof(T) * N) Vec {
   T v[N];
 };
 
-// Nearest e4m3 of x (ties to even), beyond +-448 the largest; a NaN stays one (the hardware's
-// conversion of a NaN, which the clamp alone would lose).
-__device__ __forceinline__ uint8_t to_e4m3(float x) {
-  const float c = x != x ? x : fminf(fmaxf(x, -448.f), 448.f);
-  return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, c, 0, false);
-}
-
-// Chunk of U elements: as fp32, and back.
-template <typename S, int U>
-__device__ __forceinline__ void load_chunk(const S* p, float* x) {
-  const Vec<S, U> c = *reinterpret_cast<const Vec<S, U>*>(p);
-#pragma unroll
-  for (int e = 0; e < U; ++e) x[e] = (float)c.v[e];
-}
+// Chunk of U elements as S, and in 8 bits.
 template <typename S, int U>
 __device__ __forceinline__ void store_chunk(S* p, const float* x) {
   Vec<S, U> c;
@@ -57,92 +54,179 @@ __device__ __forceinline__ void store_chunk(S* p, const float* x) {
   for (int e = 0; e < U; ++e) c.v[e] = (S)x[e];
   *reinterpret_cast<Vec<S, U>*>(p) = c;
 }
+// (Nearest e4m3, ties to even, beyond +-448 the largest; a NaN stays one.  The conversion makes
+// NaNs of values out of range, so those are clamped first, where there are any: a clamp that
+// keeps NaNs costs four instructions an element.)
 template <int U>
-__device__ __forceinline__ void store_e4m3(uint8_t* p, const float* x, float scale) {
-  Vec<uint8_t, U> c;
+__device__ __forceinline__ void store_e4m3(uint8_t* p, float* x, float inv) {
+  float most = 0.f;
 #pragma unroll
-  for (int e = 0; e < U; ++e) c.v[e] = to_e4m3(x[e] / scale);
-  *reinterpret_cast<Vec<uint8_t, U>*>(p) = c;
+  for (int e = 0; e < U; ++e) {
+    x[e] *= inv;
+    most = fmaxf(most, fabsf(x[e]));
+  }
+  if (most > 448.f) {
+#pragma unroll
+    for (int e = 0; e < U; ++e) x[e] = x[e] > 448.f ? 448.f : x[e] < -448.f ? -448.f : x[e];
+  }
+  Vec<int, U / 4> c;
+#pragma unroll
+  for (int e = 0; e < U / 4; ++e) {
+    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * e], x[4 * e + 1], 0, false);
+    c.v[e] = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * e + 2], x[4 * e + 3], w, true);
+  }
+  *reinterpret_cast<Vec<int, U / 4>*>(p) = c;
 }
 
-// Block (row t, sub-layer i).  Unit u of a row: two chunks of U elements of one head, which a
-// thread turns together: pairs (j, j + rot / 2) chunk by chunk, neighbouring pairs and the
-// dimensions that are not turned as two consecutive chunks.
+constexpr int MAX_ROWS = 8;           // per block
+
+// Block (rows of one kind, sub-layer).  Unit: two chunks of U elements of one head.  Where pairs
+// are (j, j + rot / 2), the chunks of the two halves of the rotated dimensions, which a thread
+// turns together; of other dimensions, too, one of each half, so that neighbouring threads read
+// and write neighbouring chunks.  What a thread reads first is on its way before the block looks
+// positions and pages up and forms the angles.
 template <typename S, bool E4M3, int U>
 __global__ __launch_bounds__(256) void append_kernel(AppendParams p) {
-  __shared__ float cs[MAX_FREQ], sn[MAX_FREQ];
-  const int t = blockIdx.x, i = blockIdx.y, tid = threadIdx.x;
-  const int pos = p.pos[t];
-  if (pos < 0) return;
-  const int page = paged_page(p.cache, p.seq ? p.seq[t] : t, pos);
-  if (page < 0) {
-    if (tid == 0 && p.fault) *p.fault = 1;
-    return;
-  }
-  if (tid < p.rot / 2) {
-    const double turns = (double)pos * p.turns[tid];
-    sincospif(2.f * (float)(turns - rint(turns)), &sn[tid], &cs[tid]);
-  }
-  __syncthreads();
-  const int per_head = p.hd / (2 * U), half = p.rot / 2;
-  const int nq = p.q.data ? p.heads : 0, nkv = p.cache.heads;
-  const int place = pos - (int)div_of(p.cache.page, (uint32_t)pos) * (int)p.cache.page.d;
-  for (int u = tid; u < (nq + 2 * nkv) * per_head; u += 256) {
-    const int head = u / per_head, w = u % per_head;
-    const int kind = head < nq ? 0 : head < nq + nkv ? 1 : 2;          // q, k, v
-    const int h = kind == 0 ? head : kind == 1 ? head - nq : head - nq - nkv;
-    const RowsView& src = kind == 0 ? p.q : kind == 1 ? p.k : p.v;
-    const S* in = static_cast<const S*>(src.data) + i * src.sub + t * src.row + h * p.hd;
-    const bool turn = kind != 2 && w * 2 * U < p.rot;
-    const bool halves = turn && !p.neighbours;
-    const int ca = halves ? w * U : w * 2 * U, cb = halves ? half + w * U : ca + U;
+  __shared__ float cs[MAX_ROWS][MAX_FREQ], sn[MAX_ROWS][MAX_FREQ];
+  __shared__ int64_t s_at[MAX_ROWS];  // element of the row's place in the cache, head 0; -1: none
+  const int i = blockIdx.y, tid = threadIdx.x;
+  const int kind = blockIdx.x < p.part[1].first ? 0 : blockIdx.x < p.part[2].first ? 1 : 2;
+  const Part& part = p.part[kind];
+  const int t0 = (blockIdx.x - part.first) * part.rows;
+  const int rows = min(part.rows, p.T - t0), half = p.rot / 2;
+  const int per_head = p.hd / (2 * U), log_per_head = 31 - __builtin_clz(per_head);
+  const int nkv = p.cache.heads;
+  const bool all = kind == 2 || p.neighbours;          // halves of a head, whatever is turned
+  const S* in = static_cast<const S*>(part.in.data) + i * part.in.sub + t0 * part.in.row;
+  S* out = static_cast<S*>(part.out.data);
+  if (out) out += i * part.out.sub + t0 * part.out.row;
+
+  struct Unit {
+    int row, h, ca, cb;               // the chunks' dimensions of head h
+    float scale;                      // E4M3, of keys and values
+    Vec<S, U> a, b;
+  };
+  auto fetch = [&](int x) {
+    Unit u;
+    u.row = (int)div_of(part.per_row, (uint32_t)x);
+    const int in_row = x - u.row * part.units, w = in_row & (per_head - 1);
+    u.h = in_row >> log_per_head;
+    // the first and half the number of the dimensions that are shared out
+    const bool turned = w * U < half;
+    u.ca = all || turned ? w * U : p.rot + w * U - half;
+    u.cb = u.ca + (all ? p.hd : turned ? p.rot : p.hd - p.rot) / 2;
+    if constexpr (E4M3)
+      if (kind != 0) u.scale = p.cache.scales[(i * 2 + kind - 1) * nkv + u.h];
+    const S* src = in + u.row * part.in.row + u.h * p.hd;
+    u.a = *reinterpret_cast<const Vec<S, U>*>(src + u.ca);
+    u.b = *reinterpret_cast<const Vec<S, U>*>(src + u.cb);
+    return u;
+  };
+  auto finish = [&](const Unit& u) {
+    const int64_t at = s_at[u.row];
+    if (at < 0) return;
     float a[U], b[U];
-    load_chunk<S, U>(in + ca, a);
-    load_chunk<S, U>(in + cb, b);
-    if (halves) {
 #pragma unroll
-      for (int e = 0; e < U; ++e) {
-        const float c = cs[ca + e], s = sn[ca + e], x = a[e], y = b[e];
-        a[e] = x * c - y * s;
-        b[e] = x * s + y * c;
-      }
-    } else if (turn) {
-#pragma unroll
-      for (int e = 0; e < U; e += 2) {
-        const int j = (ca + e) / 2, l = (cb + e) / 2;
-        const float x = a[e], y = a[e + 1], z = b[e], r = b[e + 1];
-        a[e] = x * cs[j] - y * sn[j];
-        a[e + 1] = x * sn[j] + y * cs[j];
-        b[e] = z * cs[l] - r * sn[l];
-        b[e + 1] = z * sn[l] + r * cs[l];
-      }
+    for (int e = 0; e < U; ++e) {
+      a[e] = (float)u.a.v[e];
+      b[e] = (float)u.b.v[e];
     }
-    const RowsView& dst = kind == 0 ? p.q_out : p.k_out;
-    if (kind != 2 && dst.data) {
-      S* out = static_cast<S*>(dst.data) + i * dst.sub + t * dst.row + h * p.hd;
-      store_chunk<S, U>(out + ca, a);
-      store_chunk<S, U>(out + cb, b);
+    if (kind != 2) {
+      if (!p.neighbours) {
+        if (u.ca < half) {
+#pragma unroll
+          for (int e = 0; e < U; ++e) {
+            const float c = cs[u.row][u.ca + e], s = sn[u.row][u.ca + e], x = a[e], y = b[e];
+            a[e] = x * c - y * s;
+            b[e] = x * s + y * c;
+          }
+        }
+      } else {
+        auto turn = [&](float* x, int first) {
+          if (first >= p.rot) return;
+#pragma unroll
+          for (int e = 0; e < U; e += 2) {
+            const int j = (first + e) / 2;
+            const float c = cs[u.row][j], s = sn[u.row][j], y = x[e], z = x[e + 1];
+            x[e] = y * c - z * s;
+            x[e + 1] = y * s + z * c;
+          }
+        };
+        turn(a, u.ca);
+        turn(b, u.cb);
+      }
+      if (out) {
+        S* dst = out + u.row * part.out.row + u.h * p.hd;
+        store_chunk<S, U>(dst + u.ca, a);
+        store_chunk<S, U>(dst + u.cb, b);
+      }
     }
     if (kind != 0) {
-      const int64_t at = (paged_row(p.cache, i, kind - 1, page, h) + place) * p.hd;
+      const int64_t to = at + (uint32_t)u.h * p.cache.page.d * (uint32_t)p.hd;
       if constexpr (E4M3) {
-        const float scale = p.cache.scales[(i * 2 + kind - 1) * nkv + h];
-        uint8_t* out = static_cast<uint8_t*>(p.cache.data) + at;
-        store_e4m3<U>(out + ca, a, scale);
-        store_e4m3<U>(out + cb, b, scale);
+        const float inv = 1.f / u.scale;
+        uint8_t* dst = static_cast<uint8_t*>(p.cache.data) + to;
+        store_e4m3<U>(dst + u.ca, a, inv);
+        store_e4m3<U>(dst + u.cb, b, inv);
       } else {
-        S* out = static_cast<S*>(p.cache.data) + at;
-        store_chunk<S, U>(out + ca, a);
-        store_chunk<S, U>(out + cb, b);
+        S* dst = static_cast<S*>(p.cache.data) + to;
+        store_chunk<S, U>(dst + u.ca, a);
+        store_chunk<S, U>(dst + u.cb, b);
       }
     }
+  };
+
+  const int total = rows * part.units;
+  int x = tid;
+  Unit u;
+  if (x < total) u = fetch(x);
+  // the rows' places, and the angles
+  for (int a = tid; a < rows * MAX_FREQ; a += 256) {
+    const int r = a / MAX_FREQ, j = a % MAX_FREQ, t = t0 + r;
+    if (j > 0 && (kind == 2 || j >= half)) continue;
+    const int pos = p.pos[t];
+    if (j == 0) {
+      int64_t at = -1;
+      if (pos >= 0) {
+        const int page = paged_page(p.cache, p.seq ? p.seq[t] : t, pos);
+        if (page < 0 && p.fault) *p.fault = 1;
+        const int place = pos - (int)(div_of(p.cache.page, (uint32_t)pos) * p.cache.page.d);
+        if (page >= 0) at = (paged_row(p.cache, i, kind == 2, page, 0) + place) * p.hd;
+      }
+      s_at[r] = at;
+    }
+    if (j < half && pos >= 0 && kind != 2) {
+      const double turns = (double)pos * p.turns[j];
+      sincospif(2.f * (float)(turns - rint(turns)), &sn[r][j], &cs[r][j]);
+    }
+  }
+  __syncthreads();
+  while (x < total) {
+    finish(u);
+    x += 256;
+    if (x < total) u = fetch(x);
   }
 }
 
 template <typename S, bool E4M3>
-hipError_t launch_append(const AppendParams& p, hipStream_t s) {
-  const dim3 grid((unsigned)p.T, (unsigned)p.cache.n);
-  hipLaunchKernelGGL((append_kernel<S, E4M3, 4>), grid, dim3(256), 0, s, p);
+hipError_t launch_append(AppendParams p, int heads, hipStream_t s) {
+  const int U = sizeof(S) == 2 && p.rot % 16 == 0 ? 8 : 4;
+  // One unit per thread: rows for 256 units (8192 rows of 8 x 48 heads of 128, with 512 and 1024
+  // units a block: 343, 351 and 359 us), fewer where not every CU had two blocks of each kind.
+  const int spread = (int)std::max<int64_t>(1, (int64_t)p.T * p.cache.n / 512);
+  unsigned blocks = 0;
+  for (int k = 0; k < 3; ++k) {
+    Part& part = p.part[k];
+    part.first = blocks;
+    part.units = (k == 0 ? heads : p.cache.heads) * (p.hd / (2 * U));
+    part.per_row = fast_div((uint32_t)part.units);
+    part.rows = std::max(1, std::min({MAX_ROWS, 256 / part.units, spread}));
+    if (part.in.data) blocks += (unsigned)((p.T + part.rows - 1) / part.rows);
+  }
+  const dim3 grid(blocks, (unsigned)p.cache.n);
+  if (U == 4) hipLaunchKernelGGL((append_kernel<S, E4M3, 4>), grid, dim3(256), 0, s, p);
+  else if constexpr (sizeof(S) == 2)
+    hipLaunchKernelGGL((append_kernel<S, E4M3, 8>), grid, dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
@@ -273,17 +357,18 @@ kraken_status kraken_op_paged_append(int32_t dtype, const kraken_rows* q, const 
     p.turns[j] = inv_freq[j] * 0.15915494309189533577;     // 1 / (2 pi)
   }
   if (T == 0) return KRAKEN_OK;
-  p.q = rows_view(q); p.k = rows_view(k); p.v = rows_view(v);
-  p.q_out = rows_view(q_out); p.k_out = rows_view(k_out);
+  p.part[0].in = rows_view(q); p.part[1].in = rows_view(k); p.part[2].in = rows_view(v);
+  p.part[0].out = rows_view(q_out); p.part[1].out = rows_view(k_out);
+  p.part[2].out = rows_view(nullptr);
   p.pos = pos; p.seq = seq; p.fault = fault;
-  p.T = T; p.heads = n_heads; p.hd = cache->head_dim; p.rot = rot_dim;
+  p.T = T; p.hd = cache->head_dim; p.rot = rot_dim;
   p.neighbours = neighbours != 0;
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e;
-  if (dtype == KRAKEN_DTYPE_F32) e = launch_append<float, false>(p, s);
+  if (dtype == KRAKEN_DTYPE_F32) e = launch_append<float, false>(p, n_heads, s);
   else if (dtype == KRAKEN_DTYPE_BF16)
-    e = e4m3 ? launch_append<bf16, true>(p, s) : launch_append<bf16, false>(p, s);
-  else e = e4m3 ? launch_append<f16, true>(p, s) : launch_append<f16, false>(p, s);
+    e = e4m3 ? launch_append<bf16, true>(p, n_heads, s) : launch_append<bf16, false>(p, n_heads, s);
+  else e = e4m3 ? launch_append<f16, true>(p, n_heads, s) : launch_append<f16, false>(p, n_heads, s);
   if (e == hipSuccess) return KRAKEN_OK;
   return fail(KRAKEN_ERR_HIP, hipGetErrorString(e));
 }
