@@ -564,43 +564,42 @@ def _check_gpu(name: str, t: torch.Tensor, device: Optional[torch.device]) -> No
         raise ValueError(f"{name} is on {t.device}, expected {device}")
 
 
-def _check_current(device: torch.device) -> None:
-    if device.index != torch.cuda.current_device():
+def _launch_stream(device: torch.device, stream) -> Optional[int]:
+    """Address of `stream`, by default the current stream of `device`, which must be the current
+    device.  (Single tokens wait for the host: this takes a tenth of torch.cuda.current_stream.)"""
+    index = torch.cuda.current_device()
+    if device.index != index:
         raise ValueError(f"the tensors are on {device}, which is not the current device")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(index) or None
+    return stream.cuda_stream or None
+
+
+def _refuse(name: str, t: torch.Tensor, dtype: torch.dtype, shape, device) -> None:
+    _check_gpu(name, t, device)
+    raise ValueError(f"{name} must have dtype {dtype} and shape {tuple(shape)} "
+                     f"(got {t.dtype}, {tuple(t.shape)})")
 
 
 def _rows(name: str, t: torch.Tensor, dtype: torch.dtype, shape, device) -> _Rows:
     """Rows [n][T][width] for the C ABI: elements of a row are adjacent, any other strides."""
-    _check_gpu(name, t, device)
-    if t.dtype != dtype:
-        raise ValueError(f"{name} must have dtype {dtype} (got {t.dtype})")
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    if t.dtype != dtype or t.shape != shape or t.device != device:
+        _refuse(name, t, dtype, shape, device)
     sub, row, col = t.stride()
     if col != 1:
         raise ValueError(f"the elements of {name}'s rows must be adjacent")
     return _Rows(t.data_ptr(), sub, row)
 
 
-def _ints(name: str, t: Optional[torch.Tensor], shape, device) -> Optional[int]:
-    """Address of a contiguous int32 GPU tensor (None: NULL)."""
+def _flat(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape,
+          device) -> Optional[int]:
+    """Address of a contiguous GPU tensor (None: NULL)."""
     if t is None:
         return None
-    _check_gpu(name, t, device)
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} "
-                         f"(got {t.dtype} {tuple(t.shape)})")
-    return t.data_ptr()
-
-
-def _floats(name: str, t: Optional[torch.Tensor], shape, device) -> Optional[int]:
-    """Address of a contiguous float32 GPU tensor (None: NULL)."""
-    if t is None:
-        return None
-    _check_gpu(name, t, device)
-    if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous float32 tensor of shape {shape} "
-                         f"(got {t.dtype} {tuple(t.shape)})")
+    if t.dtype != dtype or t.shape != shape or t.device != device:
+        _refuse(name, t, dtype, shape, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
@@ -623,7 +622,7 @@ def _paged(pages: torch.Tensor, table: torch.Tensor, scales: Optional[torch.Tens
     seqs, per_seq = table.shape
     ld = table.stride(0) if seqs > 1 else per_seq
     return _PagedCache(pages.data_ptr(), table.data_ptr(),
-                       _floats("scales", scales, (n, 2, heads), device), code, n, heads, hd,
+                       _flat("scales", scales, torch.float32, (n, 2, heads), device), code, n, heads, hd,
                        num_pages, page_size, seqs, per_seq, ld)
 
 
@@ -705,14 +704,15 @@ def op_paged_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
                 or not inv_freq.is_contiguous():
             raise ValueError("inv_freq must be a contiguous float64 vector on the host")
         freq, rot = inv_freq.data_ptr(), 2 * inv_freq.numel()
-    fault_at = _ints("fault", fault, (1,), device)
-    pos_at, seq_at = _ints("pos", pos, (T,), device), _ints("seq", seq, (T,), device)
-    _check_current(device)
+    fault_at = _flat("fault", fault, torch.int32, (1,), device)
+    pos_at = _flat("pos", pos, torch.int32, (T,), device)
+    seq_at = _flat("seq", seq, torch.int32, (T,), device)
+    at = _launch_stream(device, stream)
     if T == 0:
         return q_out
     _check(lib().kraken_op_paged_append(code, rq, rk, rv, ro, rko, T, heads, pos_at, seq_at,
                                         freq, rot, 1 if neighbours else 0, cache, fault_at,
-                                        _stream(stream)))
+                                        at))
     return q_out
 
 
@@ -733,19 +733,19 @@ def op_paged_attention(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor
         raise ValueError(f"q cannot have dtype {q.dtype}")
     shape = (cache.n_sub, cache.num_seqs, q.shape[2])
     rq = _rows("q", q, q.dtype, shape, device)
-    lens_at = _ints("lens", lens, (cache.num_seqs,), device)
-    if lens_at is None:
+    if lens is None:
         raise ValueError("lens is None")
-    fault_at = _ints("fault", fault, (1,), device)
+    lens_at = _flat("lens", lens, torch.int32, (cache.num_seqs,), device)
+    fault_at = _flat("fault", fault, torch.int32, (1,), device)
     heads = q.shape[2] // hd
     if out is None:
         out = _new(shape, q.dtype, device, stream)
     ro = _rows("out", out, q.dtype, shape, device)
     need = lib().kraken_paged_attention_work_floats(cache, heads, max_len)
     work, work_at, floats = _work(need, work, device, stream)
-    _check_current(device)
+    at = _launch_stream(device, stream)
     _check(lib().kraken_op_paged_attention(code, rq, ro, heads, cache, lens_at, max_len, scale,
-                                           work_at, floats, fault_at, _stream(stream)))
+                                           work_at, floats, fault_at, at))
     return out
 
 
@@ -778,7 +778,7 @@ def op_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = Non
     if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits must be [rows][vocab] with adjacent elements")
     rows, vocab = logits.shape
-    tokens_at = _ints("tokens", tokens, (rows,), device)
+    tokens_at = _flat("tokens", tokens, torch.int32, (rows,), device)
     if not 0 <= top <= min(vocab, MAX_TOP):
         raise ValueError(f"top must be in 0..min(vocab, {MAX_TOP})")
     logprob = None if tokens is None else _new((rows,), torch.float32, device, stream)
@@ -787,12 +787,12 @@ def op_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = Non
     best = _new((rows, top), torch.float32, device, stream) if top else None
     need = lib().kraken_token_logprobs_work_floats(rows, vocab, top)
     work, work_at, floats = _work(need, work, device, stream)
-    _check_current(device)
+    at = _launch_stream(device, stream)
     if rows:
         _check(lib().kraken_op_token_logprobs(
             code, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab,
             tokens_at, _ptr(logprob), entropy.data_ptr(), top, _ptr(ids), _ptr(best), work_at,
-            floats, _stream(stream)))
+            floats, at))
     return TokenLogprobs(logprob, entropy, ids, best)
 
 
