@@ -193,7 +193,7 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
   __shared__ int pg[4][NT * 64];                               // pages of a tile's rows
   __shared__ uint64_t row_at[NT * 64];                         // and where its K rows lie
   __shared__ int s_len[KRAKEN_MAX_SEQS];                       // keys, -1: out of range
-  extern __shared__ __align__(16) uint8_t q_rows[];            // [2][q_slot]
+  extern __shared__ __align__(16) uint8_t q_rows[];            // a unit's queries
 
   const int lane = threadIdx.x, w = blockIdx.x, g = lane >> 4, col = lane & 15;
   const int B = p.cache.seqs, U = (int)p.per_seq.d;
@@ -298,7 +298,6 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
   const uint32_t page_bytes = (uint32_t)p.cache.heads * p.cache.page.d * T::RB;
   const uint64_t v_off = (uint64_t)p.cache.pages * page_bytes;
   const uint32_t kv_at = lds_addr(kv), q_at = lds_addr(q_rows);
-  const uint32_t q_step = q_slot(p.qh, RBQ);
   // this lane's chunk of a DMA instruction's K and V rows: bytes behind the row's beginning
   uint32_t k_off[T::NI];
   uint64_t v_at[T::NI];
@@ -318,16 +317,17 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
       dma4(lds_addr(&pg[slot][x * 64]), row + div_of(p.cache.page, (uint32_t)key));
     }
   };
-  // a tile's rows, behind the queries of a unit that begins with it
-  auto fetch = [&](Place& c, int slot, int stage, bool first) {
-    if (c.j == 0 || first) {
-      const int nh = min(16, p.group - c.qb * 16);
-      const uint64_t src = reinterpret_cast<uint64_t>(
-          static_cast<const S*>(p.q.data) + c.i * p.q.sub + c.b * p.q.row +
-          (int64_t)(c.h * p.group + c.qb * 16) * HD);
-      for (int x = 0; x < nh * RBQ; x += 1024)
-        dma16(uniform((int)(q_at + stage * q_step + x)), src + min(x + lane * 16, nh * RBQ - 16));
-    }
+  // a unit's queries, adjacent rows
+  auto fetch_q = [&](const Place& c) {
+    const int bytes = min(16, p.group - c.qb * 16) * RBQ;
+    const uint64_t src = reinterpret_cast<uint64_t>(
+        static_cast<const S*>(p.q.data) + c.i * p.q.sub + c.b * p.q.row +
+        (int64_t)(c.h * p.group + c.qb * 16) * HD);
+    for (int x = 0; x < bytes; x += 1024)
+      dma16(uniform((int)(q_at + x)), src + min(x + lane * 16, bytes - 16));
+  };
+  // a tile's rows
+  auto fetch = [&](Place& c, int slot, int stage) {
     const uint64_t base = reinterpret_cast<uint64_t>(p.cache.data) + 2 * c.i * v_off +
                           (uint64_t)((uint32_t)c.h * p.cache.page.d * T::RB);
     bool bad = false;
@@ -360,10 +360,10 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
   int h0 = 0, nh = 0, bad = 0;
   bool began = false;
 
-  auto open_unit = [&](const Place& c, int stage) {
+  auto open_unit = [&](const Place& c) {
     h0 = c.h * p.group + c.qb * 16;
     nh = min(16, p.group - c.qb * 16);
-    const uint32_t src = q_at + stage * q_step + min(col, nh - 1) * RBQ;
+    const uint32_t src = q_at + min(col, nh - 1) * RBQ;
     const bool mine = col < nh;
     if constexpr (F32) {
 #pragma unroll
@@ -603,9 +603,10 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
     }
   };
 
-  // The run.  Memory operations in order: pages of tiles 0 and 1, then rows of tile t and pages
-  // of tile t + 2, tile after tile; while tile t is computed, the rows of t + 1 and the pages of
-  // t + 2 and t + 3 may be outstanding.
+  // The run.  Memory operations in order: pages of tiles 0 and 1, the first queries, then rows of
+  // tile t and pages of tile t + 2, tile after tile; while tile t is computed, the rows of t + 1
+  // and the pages of t + 2 and t + 3 may be outstanding.  The queries of a unit that begins with
+  // tile t + 1 follow the pages of t + 3, once those of tile t's unit are in registers.
   Place cur, nxt, tp2;                       // tiles t, t + 1 and t + 2
   cur = tp;
   look_up(tp, 0);
@@ -616,24 +617,37 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
     advance(tp);
   }
   tp2 = tp;
+  fetch_q(cur);
   wait_vm<0>();
-  fetch(cur, 0, 0, true);
+  fetch(cur, 0, 0);
   if (cnt > 2) {
     look_up(tp, 2);
     advance(tp);
   }
-  if (cnt > 1) fetch(nxt, 1, 1, false);
+  if (cnt > 1) fetch(nxt, 1, 1);
   if (cnt > 3) {
     look_up(tp, 3);
   }
   Place tp3 = tp;                            // tile t + 3
   for (int t = 0; t < cnt; ++t) {
     const int rem = cnt - t;
-    if (rem > 3) wait_vm<ND + 2 * NT>();
-    else if (rem == 3) wait_vm<ND + NT>();
-    else if (rem == 2) wait_vm<ND>();
-    else wait_vm<0>();
-    if (t == 0 || cur.j == 0) open_unit(cur, t & 1);
+    const bool opens = t == 0 || cur.j == 0;
+    if (rem > 3) {
+      // (a unit's queries are older than the rows of t + 1 and the pages of t + 3 alone)
+      if (opens) wait_vm<ND + NT>();
+      else wait_vm<ND + 2 * NT>();
+    } else if (rem == 3) {
+      wait_vm<ND>();
+    } else if (rem == 2) {
+      wait_vm<ND>();
+    } else {
+      wait_vm<0>();
+    }
+    if (opens) open_unit(cur);
+    if (rem > 1 && nxt.j == 0) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (the queries' reads)
+      fetch_q(nxt);
+    }
     compute(cur, t & 1);
     if (cur.j == cur.nt - 1 || rem == 1) close_unit(cur, begin + t);
     cur = nxt;
@@ -643,7 +657,7 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (rem > 3) wait_vm<ND + NT>();
       else wait_vm<ND>();
-      fetch(nxt, (t + 2) & 3, t & 1, false);
+      fetch(nxt, (t + 2) & 3, t & 1);
       tp2 = tp3;
       if (rem > 4) {
         advance(tp3);
@@ -745,9 +759,10 @@ Shape shape_of(const kraken_paged_cache* c, int n_heads, int max_len) {
   const int group = n_heads / c->n_kv_heads;
   s.qh = std::min(16, group);
   s.qblocks = (group + 15) / 16;
-  s.q_bytes = 2 * q_slot(s.qh, c->head_dim * std::max(es, 2));
-  // as many waves as LDS holds: 37 KB and the queries each of 160 KB per CU
-  const int most = 256 * std::min(4, 163840 / (37888 + s.q_bytes));
+  s.q_bytes = q_slot(s.qh, c->head_dim * std::max(es, 2));
+  // as many waves as LDS holds: at most 36 KB and the queries each of 160 KB per CU (four; three
+  // with 16 fp32 queries of 128)
+  const int most = 256 * std::min(4, 163840 / (36864 + s.q_bytes));
   const int64_t units = (int64_t)c->n_sub * c->n_kv_heads * s.qblocks * c->num_seqs;
   const int64_t per = (max_len + (int64_t)kt - 1) / kt;
   const bool whole = per <= WHOLE_TILES;
