@@ -563,7 +563,7 @@ size_t kraken_paged_cache_bytes(const kraken_paged_cache* cache);
  * Positions that no row names keep what they held.  Two rows of one call must not name one
  * place.  Apart from in-place rotation the buffers must not overlap.
  * A row whose seq, position or page is out of range writes nothing and sets *fault.
- * T = 0 does nothing.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ * T: 0 (does nothing) .. 4194304.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
  */
 kraken_status kraken_op_paged_append(int32_t dtype, const kraken_rows* q, const kraken_rows* k,
                                      const kraken_rows* v, const kraken_rows* q_out,
@@ -622,7 +622,8 @@ kraken_status kraken_op_paged_attention(int32_t dtype, const kraken_rows* q,
  *             kraken_op_paged_attention.
  * Computed in fp32.  A row that holds a NaN or +inf, or nothing but -inf, has no distribution:
  * its log probabilities and entropy are NaN (its top_ids are still the largest logits, a NaN
- * counting as larger than +inf).  rows = 0 does nothing.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ * counting as larger than +inf).  rows: 0 (does nothing) .. 4194304.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.
  * kraken_token_logprobs_work_floats: the scratch such a call needs; -1 for sizes that the call
  * refuses.
  */

@@ -436,7 +436,7 @@ using namespace kraken;
 extern "C" {
 
 int64_t kraken_token_logprobs_work_floats(int32_t rows, int32_t vocab, int32_t top) {
-  if (rows < 0 || vocab < 1 || top < 0 || top > KRAKEN_MAX_TOP || top > vocab) return -1;
+  if (rows < 0 || rows > 1 << 22 || vocab < 1 || top < 0 || top > KRAKEN_MAX_TOP || top > vocab) return -1;
   const int splits = splits_of(rows, vocab);
   return splits == 1 ? 0 : (int64_t)rows * splits * (4 + 2 * top);
 }
@@ -450,6 +450,7 @@ kraken_status kraken_op_token_logprobs(int32_t dtype, const void* logits, int64_
     return fail(KRAKEN_ERR_UNSUPPORTED, "unknown dtype");
   if (rows < 0 || vocab < 1 || ld < vocab)
     return fail(KRAKEN_ERR_INVALID_ARG, "bad rows, vocab or ld");
+  if (rows > 1 << 22) return fail(KRAKEN_ERR_UNSUPPORTED, "rows above 4194304");
   if (top < 0 || top > KRAKEN_MAX_TOP || top > vocab)
     return fail(KRAKEN_ERR_INVALID_ARG, "top out of 0..min(vocab, KRAKEN_MAX_TOP)");
   if (!logits) return fail(KRAKEN_ERR_INVALID_ARG, "logits is NULL");

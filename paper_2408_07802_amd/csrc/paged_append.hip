@@ -336,6 +336,7 @@ kraken_status kraken_op_paged_append(int32_t dtype, const kraken_rows* q, const 
     return fail(KRAKEN_ERR_UNSUPPORTED,
                 "the cache has the rows' dtype, or is E4M3 with BF16 or F16 rows");
   if (T < 0) return fail(KRAKEN_ERR_INVALID_ARG, "T is negative");
+  if (T > 1 << 22) return fail(KRAKEN_ERR_UNSUPPORTED, "T above 4194304");
   if (T > 0 && (!k || !v || !pos)) return fail(KRAKEN_ERR_INVALID_ARG, "k, v or pos is NULL");
   if (!q != !q_out) return fail(KRAKEN_ERR_INVALID_ARG, "q and q_out go together");
   if (n_heads < 1 || n_heads > 65535 || n_heads % cache->n_kv_heads != 0)

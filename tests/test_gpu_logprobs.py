@@ -110,6 +110,38 @@ def test_rows_without_a_distribution_and_padding():
     assert e.logprob.shape == (0,) and e.top_ids.shape == (0, 2)
 
 
+def test_rows_past_32_bit_offsets():
+    V, ld = 3000, 2 ** 31 + 12345
+    flat = torch.empty(ld + V, dtype=torch.float16, device=DEV)
+    x = flat.as_strided((2, V), (ld, 1))
+    y, tokens = make(2, V, torch.float16, 9)
+    x.copy_(y)
+    r = K.op_token_logprobs(x, tokens, top=7)
+    check(y, tokens, 7, r)
+
+
+@pytest.mark.parametrize("rows", [1, 600])
+def test_many_equal_logits(rows):
+    """Constrained decoding: a few tokens allowed, all others at -inf or the lowest value, so that
+    most of the alternatives are ties; and a row that rises to its end, where every later piece
+    is larger than all before."""
+    V = 20011
+    c = torch.arange(V, device=DEV, dtype=torch.float32)
+    for dtype in (torch.float32, torch.bfloat16):
+        x = torch.full((rows, V), -math.inf, device=DEV)
+        x[:, 5000::6007] = 1.5
+        x[0] = torch.finfo(dtype).min
+        x[0, 77] = 3.0
+        if rows > 1:
+            x[1], x[2], x[3] = c / 100, torch.floor(c / 4), -c
+        x = x.to(dtype)
+        tokens = torch.full((rows,), 77, dtype=torch.int32, device=DEV)
+        for top in (5, 64):
+            check(x, tokens.where(torch.arange(rows, device=DEV) < 4, 5000), top,
+                  K.op_token_logprobs(x, tokens.where(torch.arange(rows, device=DEV) < 4, 5000),
+                                      top=top))
+
+
 def test_workspace_graph_and_streams():
     x, tokens = make(4, 60000, torch.bfloat16, 3)
     want = K.op_token_logprobs(x, tokens, top=8)

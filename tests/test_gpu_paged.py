@@ -370,6 +370,66 @@ def test_attention_marks_bad_rows():
     assert int(fault) == 0 and bool(out.isfinite().all())
 
 
+def test_attention_of_256_sequences():
+    """More units than waves, and as many sequences as a call takes: runs that end in the middle
+    of units, rows without keys in between, a row length out of range."""
+    n, H, Hkv, hd, page, B = 3, 12, 6, 64, 24, 256
+    g = gen(30)
+    lens = [0 if b % 7 == 3 else (37 * b) % 300 for b in range(B)]
+    lens[100], lens[255] = 2500, 1
+    pages, table = make_cache(n, Hkv, hd, page, lens, torch.bfloat16, g)
+    q = normal((B, n, H * hd), torch.bfloat16, g).transpose(0, 1)       # sub-layers behind rows
+    out = torch.empty((B, n, H * hd), dtype=torch.bfloat16, device=DEV).transpose(0, 1)
+    lens_d = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    lens_d[17] = 2501
+    fault = torch.zeros(1, dtype=torch.int32, device=DEV)
+    K.op_paged_attention(q, pages, table, lens_d, 2500, out, fault=fault)
+    assert int(fault) == 1
+    lens[17] = 0
+    ref, slack = attention64(q, pages, table, lens, None, 0.125, hd)
+    assert bool(out[:, 17].isnan().all())
+    keep = torch.arange(B, device=DEV) != 17
+    near(out[:, keep], ref[:, keep], slack[:, keep], "256")
+
+
+def test_a_table_of_wider_rows_and_a_cache_past_32_bit_offsets():
+    """Pages at the far end of a cache of 6.4 GB (2^31.7 elements a sub-layer), named by the left
+    part of a wider table: append there, attend there, and nothing else is touched."""
+    n, H, hd, page, B = 2, 2, 128, 64, 3
+    total = 24600
+    pages = torch.empty((n, 2, total, H, page, hd), dtype=torch.float16, device=DEV)
+    wide = torch.full((B, 40), -1, dtype=torch.int32, device=DEV)
+    table = wide[:, :5]
+    far = torch.arange(total - 15, total, dtype=torch.int32, device=DEV).flip(0).view(B, 5)
+    table.copy_(far)
+    g = gen(31)
+    lens = [300, 1, 129]
+    T = sum(lens)
+    d = H * hd
+    x = normal((n, T, 3 * d), torch.float16, g)
+    seq = torch.repeat_interleave(torch.arange(B), torch.tensor(lens)).to(torch.int32).to(DEV)
+    pos = torch.cat([torch.arange(v, dtype=torch.int32) for v in lens]).to(DEV)
+    low = pages[:, :, :8].clone()
+    fault = torch.zeros(1, dtype=torch.int32, device=DEV)
+    K.op_paged_append(x[..., :d], x[..., d:2 * d], x[..., 2 * d:], pages, table, pos, seq=seq,
+                      fault=fault)
+    new = normal((n, B, d), torch.float16, g)
+    out = K.op_paged_attention(new, pages, table, torch.tensor(lens, dtype=torch.int32,
+                                                               device=DEV), 300, fault=fault)
+    assert int(fault) == 0
+    assert torch.equal(pages[:, :, :8].view(torch.int16), low.view(torch.int16))
+    at = 0
+    for b, L in enumerate(lens):
+        rows = pages[:, :, table[b].long()].transpose(2, 3).reshape(n, 2, H, -1, hd)[:, :, :, :L]
+        for j in (0, 1):
+            want = x[:, at:at + L, (1 + j) * d:(2 + j) * d].unflatten(-1, (H, hd)).transpose(1, 2)
+            assert torch.equal(rows[:, j], want)
+        at += L
+    small, ids = pages[:, :, total - 15:].contiguous(), (table - (total - 15)).contiguous()
+    ref, slack = attention64(new, small, ids, lens, None, hd ** -0.5, hd)
+    near(out, ref, slack, "far pages")
+
+
 def test_sequences_share_pages():
     g = gen(8)
     pages, table = make_cache(1, 2, 64, 16, [100], torch.bfloat16, g)

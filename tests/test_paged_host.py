@@ -35,6 +35,7 @@ BAD_CACHES = [
     (dict(pages_per_seq=0), INVALID), (dict(table_ld=3), INVALID),
     (dict(pages_per_seq=1 << 27, table_ld=1 << 27), INVALID),
     (dict(n_sub=65535, n_kv_heads=65535, num_pages=2 ** 31 - 1), INVALID),
+    (dict(page_size=1 << 24, pages_per_seq=1, table_ld=1), UNSUPPORTED),    # 2^32 bytes a page
 ]
 BAD_POINTERS = [
     (dict(pages=None), INVALID), (dict(table=None), INVALID), (dict(pages=A + 8), INVALID),
@@ -72,6 +73,7 @@ def test_bad_caches_are_refused(kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(dtype=3), UNSUPPORTED), (dict(dtype=-1), UNSUPPORTED),
     (dict(dtype=K.DTYPE_BF16), UNSUPPORTED), (dict(T=-1), INVALID), (dict(T=4), INVALID),
+    (dict(T=4194305, seq=A), UNSUPPORTED),
     (dict(k=None), INVALID), (dict(v=None), INVALID), (dict(pos=None), INVALID),
     (dict(q=None), INVALID), (dict(q_out=None), INVALID), (dict(heads=0), INVALID),
     (dict(heads=3), INVALID), (dict(rot=4), INVALID), (dict(rot=72), INVALID),
@@ -110,6 +112,7 @@ def test_attention_refuses(kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(dtype=3), UNSUPPORTED), (dict(logits=None), INVALID), (dict(logits=A + 2), INVALID),
     (dict(rows=-1), INVALID), (dict(vocab=0), INVALID), (dict(ld=99), INVALID),
+    (dict(rows=4194305), UNSUPPORTED),
     (dict(top=-1), INVALID), (dict(top=65), INVALID), (dict(top=5, vocab=4, ld=4), INVALID),
     (dict(tokens=None), INVALID), (dict(logprob=None), INVALID), (dict(ids=None), INVALID),
     (dict(best=None), INVALID), (dict(top=0), INVALID), (dict(work=A + 4), INVALID),
@@ -123,6 +126,14 @@ def test_logprobs_refuse(kw, status):
         a["dtype"], a["logits"], a["ld"], a["rows"], a["vocab"], a["tokens"], a["logprob"],
         a["entropy"], a["top"], a["ids"], a["best"], a["work"], a["floats"], None) == status
     assert K.lib().kraken_last_error()
+
+
+def test_attention_refuses_2_31_tiles():
+    # 65535 sub-layers of 2 heads of 256 sequences of 4097 keys: 65 tiles of 64 keys each
+    c = cache(n_sub=65535, num_seqs=256, pages_per_seq=257, table_ld=257)
+    assert 65535 * 2 * 256 * 65 >= 2 ** 31
+    assert attention(c=c, max_len=4097) == UNSUPPORTED
+    assert b"tiles" in K.lib().kraken_last_error()
 
 
 def test_sizes():
