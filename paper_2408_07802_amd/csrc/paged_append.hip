@@ -210,7 +210,9 @@ __global__ __launch_bounds__(256) void append_kernel(AppendParams p) {
 
 template <typename S, bool E4M3>
 hipError_t launch_append(AppendParams p, int heads, hipStream_t s) {
-  const int U = sizeof(S) == 2 && p.rot % 16 == 0 ? 8 : 4;
+  // 16 bytes of a 16-bit row at a time, unless half the rotated dimensions end inside of them
+  // (heads of 104: 8 bytes)
+  const int U = sizeof(S) == 2 && (p.neighbours || p.rot % 16 == 0) ? 8 : 4;
   // One unit per thread: rows for 256 units (8192 rows of 8 x 48 heads of 128, with 512 and 1024
   // units a block: 343, 351 and 359 us), fewer where not every CU had two blocks of each kind.
   const int spread = (int)std::max<int64_t>(1, (int64_t)p.T * p.cache.n / 512);

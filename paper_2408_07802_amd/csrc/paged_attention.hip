@@ -15,8 +15,9 @@
 // lie in registers.  Only few of the 16 columns are used where few query heads share a
 // key/value head; the products are cheap next to the tile's bytes all the same.
 //
-// Data: a tile's K and V rows (8 KB each) go from the pages straight into LDS, two tiles in
-// flight, and the page numbers of a tile's rows do so two tiles before that.  Chunks of 16 bytes
+// Data: a tile's K and V rows (8 KB each) go from the pages straight into LDS, two tiles ahead
+// (K rows as soon as the scores have left their place free), and the page numbers of a tile's
+// rows do so two tiles before that.  Chunks of 16 bytes
 // of a row are permuted so that the reads spread over all LDS banks; V is read transposed
 // (ds_read_b64_tr).
 #include <hip/hip_runtime.h>
@@ -326,8 +327,8 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
     for (int x = 0; x < bytes; x += 1024)
       dma16(uniform((int)(q_at + x)), src + min(x + lane * 16, bytes - 16));
   };
-  // a tile's rows
-  auto fetch = [&](Place& c, int slot, int stage) {
+  // a tile's K rows, and then (with the rows' places as they are) its V rows
+  auto fetch_k = [&](Place& c, int slot, int stage) {
     const uint64_t base = reinterpret_cast<uint64_t>(p.cache.data) + 2 * c.i * v_off +
                           (uint64_t)((uint32_t)c.h * p.cache.page.d * T::RB);
     bool bad = false;
@@ -348,8 +349,13 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
     for (int x = 0; x < T::NI; ++x) {
       const uint64_t at = row_at[x * T::RPI + lane / T::NC];
       dma16(to + x * 1024, at + k_off[x]);
-      dma16(to + STAGE + x * 1024, at + v_at[x]);
     }
+  };
+  auto fetch_v = [&](int stage) {
+    const uint32_t to = kv_at + stage * (2 * STAGE) + STAGE;
+#pragma unroll
+    for (int x = 0; x < T::NI; ++x)
+      dma16(to + x * 1024, row_at[x * T::RPI + lane / T::NC] + v_at[x]);
   };
 
   // state of the unit at hand: the lane's query head col
@@ -400,9 +406,9 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
   // aligned bytes of a row, so the permuted chunk of block f is one exclusive or away.)
   const uint32_t k_row = kv_at + col * T::RB;
   const int k_k = k_key<C, HD>(col);
-  auto compute = [&](const Place& c, int stage) {
+  f32x4 sc[KB];                             // scores of the tile at hand
+  auto score = [&](int stage) {
     const uint32_t K = k_row + stage * (2 * STAGE);
-    f32x4 sc[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) sc[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
     if constexpr (F32) {
@@ -444,6 +450,8 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
           sc[kb] = mfma32<S>(lds_read<Vec8<S>>(at + kb * 16 * T::RB), q[m], sc[kb]);
       }
     }
+  };
+  auto output = [&](const Place& c, int stage) {
     // scores in base-2 units, of keys 16 kb + 4 g + r
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) sc[kb] *= ks;
@@ -619,12 +627,16 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
   tp2 = tp;
   fetch_q(cur);
   wait_vm<0>();
-  fetch(cur, 0, 0);
+  fetch_k(cur, 0, 0);
+  fetch_v(0);
   if (cnt > 2) {
     look_up(tp, 2);
     advance(tp);
   }
-  if (cnt > 1) fetch(nxt, 1, 1);
+  if (cnt > 1) {
+    fetch_k(nxt, 1, 1);
+    fetch_v(1);
+  }
   if (cnt > 3) {
     look_up(tp, 3);
   }
@@ -648,21 +660,26 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (the queries' reads)
       fetch_q(nxt);
     }
-    compute(cur, t & 1);
-    if (cur.j == cur.nt - 1 || rem == 1) close_unit(cur, begin + t);
-    cur = nxt;
-    nxt = tp2;
+    score(t & 1);
     if (rem > 2) {
-      // the stage's reads are done, and the page numbers are there
+      // the K rows' reads are done, and the page numbers are there
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (rem > 3) wait_vm<ND + NT>();
       else wait_vm<ND>();
-      fetch(nxt, (t + 2) & 3, t & 1);
-      tp2 = tp3;
-      if (rem > 4) {
-        advance(tp3);
-        look_up(tp3, t & 3);
-      }
+      fetch_k(tp2, (t + 2) & 3, t & 1);
+    }
+    output(cur, t & 1);
+    if (cur.j == cur.nt - 1 || rem == 1) close_unit(cur, begin + t);
+    if (rem > 2) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      fetch_v(t & 1);
+    }
+    cur = nxt;
+    nxt = tp2;
+    tp2 = tp3;
+    if (rem > 4) {
+      advance(tp3);
+      look_up(tp3, t & 3);
     }
   }
 }
@@ -671,9 +688,9 @@ __global__ __launch_bounds__(64, 1) void paged_attn_kernel(PagedAttnParams p) {
 // out = sum o e^(m - M) / sum l e^(m - M).  Block (entry of desc, share of the query heads); a
 // group of HD / 4 lanes takes a query head's partials, every gph-th of them where there are more
 // groups than heads.
-template <typename S, int HD>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p) {
-  constexpr int LQ = HD / 4, NG = 256 / LQ;
+template <typename S, int HD, int THREADS>
+__global__ __launch_bounds__(THREADS) void paged_join_kernel(PagedAttnParams p) {
+  constexpr int LQ = HD / 4, NG = THREADS / LQ;
   __shared__ float sm[NG], sl[NG];
   __shared__ f32x4 so[NG][LQ];
   const int tid = threadIdx.x, grp = tid / LQ, f = tid % LQ;
@@ -750,9 +767,15 @@ int cache_es(int dtype) {
 // How a call is shared out.
 struct Shape {
   int qh, qblocks, q_bytes, waves, entries;      // entries of desc (0: whole units)
+  int parts;                                     // of a unit, about, at most
   double tiles;                                  // at most
 };
+// Units of up to 4 tiles are not shared: a wave takes 1.2 to 1.9 us a tile (after 4.3 us for the
+// first), the join 5 us.
 constexpr int WHOLE_TILES = 4;
+// Tiles of a run, at least, once that leaves a wave for every CU (65536 keys of one head: 41 us
+// with runs of two tiles).
+constexpr int RUN_TILES = 4;
 Shape shape_of(const kraken_paged_cache* c, int n_heads, int max_len) {
   Shape s;
   const int es = cache_es(c->dtype), kt = tile_keys(c->head_dim, es);
@@ -768,21 +791,27 @@ Shape shape_of(const kraken_paged_cache* c, int n_heads, int max_len) {
   const bool whole = per <= WHOLE_TILES;
   s.tiles = (double)units * per;
   const double items = (double)units * (whole ? 1 : per);
-  s.waves = items >= most ? most : std::max(1, (int)items);
+  const double want = whole ? items : std::max(std::min(items, 256.0), items / RUN_TILES);
+  s.waves = want >= most ? most : std::max(1, (int)want);
   s.entries = whole ? 0 : (int)std::min<int64_t>(units, s.waves);
+  s.parts = (int)std::min<double>(s.waves, per * (s.waves / items) + 2);
   return s;
 }
 
 template <typename S, typename C, int HD>
 hipError_t launch_hd(const PagedAttnParams& p, const Shape& sh, hipStream_t s) {
-  hipLaunchKernelGGL((paged_attn_kernel<S, C, HD>), dim3((unsigned)p.W), dim3(64),
-                     (unsigned)sh.q_bytes, s, p);
+  const dim3 grid((unsigned)p.W);
+  hipLaunchKernelGGL((paged_attn_kernel<S, C, HD>), grid, dim3(64), (unsigned)sh.q_bytes, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.whole) return e;
-  // (about 2048 blocks: more wait for the rest to start and find nothing to do)
+  // about 2048 blocks (more wait for the rest to start and find nothing to do), and more threads
+  // for each of few that have much to read
   const int y = std::max(1, std::min(sh.qh, 2048 / sh.entries));
-  hipLaunchKernelGGL((paged_join_kernel<S, HD>), dim3((unsigned)sh.entries, (unsigned)y),
-                     dim3(256), 0, s, p);
+  const dim3 joins((unsigned)sh.entries, (unsigned)y);
+  if (sh.parts > 128)
+    hipLaunchKernelGGL((paged_join_kernel<S, HD, 1024>), joins, dim3(1024), 0, s, p);
+  else
+    hipLaunchKernelGGL((paged_join_kernel<S, HD, 256>), joins, dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
