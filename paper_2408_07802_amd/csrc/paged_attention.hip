@@ -114,12 +114,17 @@ __device__ __forceinline__ float sum4(float x) {
   return q.a + q.b;
 }
 
+// Keys of a tile of rows of hd elements of es bytes: 8 KB, at most 128.  (Tiles of 4 KB with twice
+// the waves: the same for 16-bit rows of 64, 2 to 8% slower for 8-bit rows, whose instructions
+// per tile are many.)
+constexpr int tile_keys(int hd, int es) { return 8192 / (hd * es) < 128 ? 8192 / (hd * es) : 128; }
+
 // Sizes of a tile.  C: the cache's element type.
 template <typename C, int HD>
 struct Tile {
   static constexpr int RB = HD * (int)sizeof(C);               // bytes of a row
   static constexpr int NC = RB / 16;                           // 16-byte chunks of a row
-  static constexpr int KT = 8192 / RB < 128 ? 8192 / RB : 128; // keys
+  static constexpr int KT = tile_keys(HD, (int)sizeof(C));     // keys
   static constexpr int RPI = 64 / NC;                          // rows per DMA instruction
   static constexpr int NI = KT / RPI;                          // DMA instructions for K (for V)
   static constexpr int NT = (KT + 63) / 64;                    // and for the page numbers
@@ -757,9 +762,6 @@ __global__ __launch_bounds__(THREADS) void paged_join_kernel(PagedAttnParams p) 
   }
 }
 
-// Keys per tile of a cache with rows of head_dim elements of es bytes.
-int tile_keys(int head_dim, int es) { return std::min(128, 8192 / (head_dim * es)); }
-
 int cache_es(int dtype) {
   return dtype == KRAKEN_DTYPE_E4M3 ? 1 : dtype == KRAKEN_DTYPE_F32 ? 4 : 2;
 }
@@ -783,9 +785,9 @@ Shape shape_of(const kraken_paged_cache* c, int n_heads, int max_len) {
   s.qh = std::min(16, group);
   s.qblocks = (group + 15) / 16;
   s.q_bytes = q_slot(s.qh, c->head_dim * std::max(es, 2));
-  // as many waves as LDS holds: at most 36 KB and the queries each of 160 KB per CU (four; three
-  // with 16 fp32 queries of 128)
-  const int most = 256 * std::min(4, 163840 / (36864 + s.q_bytes));
+  // as many waves as LDS holds: two stages of K and V, 4 KB at most of lengths, pages and places,
+  // and the queries (four per CU; three with 16 fp32 queries of 128, seven with 8-bit heads of 32)
+  const int most = 256 * (163840 / (4 * kt * c->head_dim * es + 4096 + s.q_bytes));
   const int64_t units = (int64_t)c->n_sub * c->n_kv_heads * s.qblocks * c->num_seqs;
   const int64_t per = (max_len + (int64_t)kt - 1) / kt;
   const bool whole = per <= WHOLE_TILES;
