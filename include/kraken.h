@@ -589,10 +589,11 @@ kraken_status kraken_op_paged_append(int32_t dtype, const kraken_rows* q, const 
  *   work     device float32 scratch, 16-byte aligned, of work_floats >=
  *            kraken_paged_attention_work_floats(cache, n_heads, max_len); NULL if that is 0.
  *            It need not hold anything; calls that may run at one time need one each.
- * Sizes: the keys of all heads and sequences, if every one had max_len, fill fewer than 2^31
+ * Sizes: the keys of all heads and sequences, if every one had max_len, fill fewer than 2^30
  * tiles (8 KB of one head's keys, at most 128 keys).
  * Scores, softmax and sums are fp32.  Positions at or past lens[b] are never read.  The same
- * call gives the same bits.  A row whose length is out of range (0 .. max_len) or that needs a
+ * call gives the same bits.  A head whose scores are all -inf gives NaN, a value of +-inf an
+ * infinity or NaN.  A row whose length is out of range (0 .. max_len) or that needs a
  * page out of range gives NaN and sets *fault.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
  * kraken_paged_attention_work_floats: the scratch such a call needs; -1 for sizes that the call
  * refuses (the cache's pointers are not looked at).

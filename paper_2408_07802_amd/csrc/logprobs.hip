@@ -12,6 +12,11 @@
 // read again, their keys at or above the bound collected in LDS and ranked.  Where more keys
 // come than fit (rows of many equal logits), the block looks for a better bound by counting
 // (bisection over the 32-bit order of fp32), and takes equal logits by ascending index.
+//
+// What bounds it: many rows, the logits read once (2048 x 51200 fp32 with the likeliest token: 83
+// us, 5.1 TB/s; without alternatives 81, with 20 of them 80 to 85 us).  A few rows, one block's
+// pass over 50 000 logits: 12 us (7 us without alternatives), of which the vector units are
+// busy for half.  Ranking a running list per wave instead of the bound: 21 and 111 us.
 #include <hip/hip_runtime.h>
 #include <math.h>
 

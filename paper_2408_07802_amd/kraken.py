@@ -616,7 +616,8 @@ def _paged(pages: torch.Tensor, table: torch.Tensor, scales: Optional[torch.Tens
         raise ValueError("pages must be a contiguous tensor "
                          "[n][2][num_pages][kv_heads][page_size][head_dim]")
     _check_gpu("table", table, device)
-    if table.dtype != torch.int32 or table.dim() != 2 or table.stride(1) != 1:
+    if table.dtype != torch.int32 or table.dim() != 2 or \
+            (table.shape[1] > 1 and table.stride(1) != 1):
         raise ValueError("table must be int32 [num_seqs][pages_per_seq] with adjacent entries")
     n, _, num_pages, heads, page_size, hd = pages.shape
     seqs, per_seq = table.shape

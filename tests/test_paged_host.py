@@ -128,12 +128,16 @@ def test_logprobs_refuse(kw, status):
     assert K.lib().kraken_last_error()
 
 
-def test_attention_refuses_2_31_tiles():
-    # 65535 sub-layers of 2 heads of 256 sequences of 4097 keys: 65 tiles of 64 keys each
+def test_attention_refuses_2_30_tiles():
+    # 65535 sub-layers of 2 heads of 256 sequences of 2049 keys: 33 tiles of 64 keys each
     c = cache(n_sub=65535, num_seqs=256, pages_per_seq=257, table_ld=257)
-    assert 65535 * 2 * 256 * 65 >= 2 ** 31
-    assert attention(c=c, max_len=4097) == UNSUPPORTED
+    assert 65535 * 2 * 256 * 33 >= 2 ** 30
+    assert attention(c=c, max_len=2049) == UNSUPPORTED
     assert b"tiles" in K.lib().kraken_last_error()
+    # as many units without any key
+    c = cache(n_sub=65535, n_kv_heads=65, num_seqs=256)
+    assert attention(c=c, heads=65, max_len=0, q=rows(row=65536, sub=1 << 24),
+                     out=rows(row=65536, sub=1 << 24)) == UNSUPPORTED
 
 
 def test_sizes():
