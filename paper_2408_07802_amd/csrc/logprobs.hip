@@ -2,7 +2,8 @@
 //
 // With m the largest logit, s = sum e^(x - m) and u = sum e^(x - m) (x - m):
 //   log p(x) = (x - m) - log s,   entropy = log s - u / s.
-// Both are formed from differences to m, so an offset of the row costs no precision.  One pass:
+// Both are formed from differences to m, so an offset of the row costs no precision.  (c x - c m
+// in one operation would: its products overflow at the lowest values that masks hold.)  One pass:
 // every lane keeps its own (m, s, u), rescaled when its m grows; they are joined at the end.
 //
 // The most likely tokens: a logit and its index make a 64-bit key (larger logit, then lower
@@ -13,10 +14,10 @@
 // come than fit (rows of many equal logits), the block looks for a better bound by counting
 // (bisection over the 32-bit order of fp32), and takes equal logits by ascending index.
 //
-// What bounds it: many rows, the logits read once (2048 x 51200 fp32 with the likeliest token: 83
-// us, 5.1 TB/s; without alternatives 81, with 20 of them 80 to 85 us).  A few rows, one block's
-// pass over 50 000 logits: 12 us (7 us without alternatives), of which the vector units are
-// busy for half.  Ranking a running list per wave instead of the bound: 21 and 111 us.
+// What bounds it: many rows, the logits read once (2048 x 51200 fp32 with the likeliest token: 78
+// us, 5.4 TB/s, as without it; with 64 alternatives 84 us).  Few rows, one block's pass over
+// 50 000 logits: 12 us (8 us without alternatives), of which the vector units are busy for half.
+// A list per wave, ranked as it fills, instead of the bound: 21 and 111 us.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -149,7 +150,14 @@ __global__ __launch_bounds__(NW * 64) void logprob_kernel(LogprobParams p) {
   const int nv = (int)(((int64_t)off + p.vocab + VPT - 1) / VPT);
   const int per = (nv + p.splits - 1) / p.splits;
   const int v0 = share * per, v1 = min(v0 + per, nv);
+  const int whole = min(nv - 1, v1);          // vectors 1 .. whole - 1 lie inside the row
   auto load = [&](int first, uint4* raw) {
+    if (first > 0 && first + 64 * GV <= whole) {
+      const uint4* from = reinterpret_cast<const uint4*>(base) + first + lane;
+#pragma unroll
+      for (int g = 0; g < GV; ++g) raw[g] = from[g * 64];
+      return;
+    }
 #pragma unroll
     for (int g = 0; g < GV; ++g) {
       const int v = first + g * 64 + lane;
@@ -421,8 +429,7 @@ void launch_logprobs(const LogprobParams& p, hipStream_t s) {
 
 template <typename S>
 hipError_t launch_typed(const LogprobParams& p, hipStream_t s) {
-  // 8 blocks of 4 waves share a CU, one of 16 has it alone: many rows stream better (2048 x 51200
-  // fp32: 83 us, 5.1 TB/s), few end sooner
+  // 8 blocks of 4 waves share a CU, one of 16 has it alone: many rows stream better, few end sooner
   if (p.rows * (int64_t)p.splits >= 512) launch_logprobs<S, 4>(p, s);
   else launch_logprobs<S, 16>(p, s);
   hipError_t e = hipGetLastError();
