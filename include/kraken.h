@@ -526,7 +526,8 @@ typedef struct {
 
 /* Rows of n_sub sub-layers: element c of row t of sub-layer i at
  * data + i * sub_stride + t * row_stride + c (strides in elements, at least 0; data and the
- * strides aligned to 16 bytes).  The columns Q | K | V of one projection are three of these. */
+ * strides aligned to 16 bytes; rows that a call writes share no element).  The columns Q | K | V
+ * of one projection are three of these. */
 typedef struct {
   void* data;
   int64_t sub_stride;

@@ -60,6 +60,22 @@ KRAKEN_HD int run_length(FastDiv runs, int total) {
   return q + ((uint32_t)q * runs.d < (uint32_t)total || q == 0 ? 1 : 0);
 }
 
+// Whether two of n x T rows of `width` elements, row t of sub-layer i at i sub + t row (strides >=
+// 0), share an element.  Rows of equal i or t are a multiple of one stride apart; of rows di
+// sub-layers apart, the nearest are those whose rows lie di sub / row apart, rounded either way.
+inline bool rows_overlap(int n, int64_t T, int64_t sub, int64_t row, int64_t width) {
+  if ((n > 1 && T > 0 && sub < width) || (T > 1 && row < width)) return true;
+  if (n < 2 || T < 2) return false;
+  const __int128 rows_end = (__int128)(T - 1) * row + width, subs_end = (__int128)(n - 1) * sub + width;
+  if (sub >= rows_end || row >= subs_end) return false;    // one inside a step of the other
+  for (int di = 1; di < n; ++di) {
+    const __int128 at = (__int128)di * sub, dt = at / row;
+    if (dt < T && at - dt * row < width) return true;
+    if (dt + 1 < T && (dt + 1) * row - at < width) return true;
+  }
+  return false;
+}
+
 // Checks a cache's description (with_data: its pointers, too) and fills view; a message and
 // *status otherwise.
 const char* paged_view(const kraken_paged_cache* cache, bool with_data, PagedView* view,

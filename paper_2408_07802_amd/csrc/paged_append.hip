@@ -296,9 +296,10 @@ const char* check_rows(const kraken_rows* r, int n, int64_t T, int es,
   if (!r->data) return "rows without data";
   const int64_t sub = n > 1 ? r->sub_stride : 0, row = T > 1 ? r->row_stride : 0;
   if (sub < 0 || row < 0) return "negative stride";
-  if (reinterpret_cast<uintptr_t>(r->data) % 16 != 0 || sub * es % 16 != 0 || row * es % 16 != 0)
+  if (reinterpret_cast<uintptr_t>(r->data) % 16 != 0 || sub % (16 / es) != 0 ||
+      row % (16 / es) != 0)
     return "rows and their strides must be aligned to 16 bytes";
-  if ((n > 1 && sub < out_width) || (T > 1 && row < out_width))
+  if (out_width > 0 && rows_overlap(n, T, sub, row, out_width))
     return "the rows of an output overlap";
   return nullptr;
 }

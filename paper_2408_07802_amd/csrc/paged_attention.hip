@@ -869,6 +869,9 @@ kraken_status kraken_op_paged_attention(int32_t dtype, const kraken_rows* q,
   if (max_len < 0 || max_len > (int64_t)cache->pages_per_seq * cache->page_size)
     return fail(KRAKEN_ERR_INVALID_ARG, "max_len out of 0..pages_per_seq * page_size");
   if (!isfinite(scale)) return fail(KRAKEN_ERR_INVALID_ARG, "scale is not finite");
+  const Shape sh = shape_of(cache, n_heads, max_len);
+  if (sh.tiles >= 1073741824.0)
+    return fail(KRAKEN_ERR_UNSUPPORTED, "2^30 or more tiles of keys");
   const int es = dtype == KRAKEN_DTYPE_F32 ? 4 : 2;
   for (const kraken_rows* r : {q, out})
     if (const char* msg = check_rows(r, cache->n_sub, cache->num_seqs, es,
@@ -884,9 +887,6 @@ kraken_status kraken_op_paged_attention(int32_t dtype, const kraken_rows* q,
   p.out = {out->data, out->sub_stride, out->row_stride};
   p.lens = lens; p.fault = fault;
   p.heads = n_heads; p.group = n_heads / cache->n_kv_heads; p.max_len = max_len;
-  const Shape sh = shape_of(cache, n_heads, max_len);
-  if (sh.tiles >= 1073741824.0)
-    return fail(KRAKEN_ERR_UNSUPPORTED, "2^30 or more tiles of keys");
   p.qblocks = sh.qblocks;
   p.per_run = fast_div((uint32_t)sh.waves);
   p.per_seq = fast_div((uint32_t)(cache->n_sub * cache->n_kv_heads * sh.qblocks));

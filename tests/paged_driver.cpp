@@ -1,6 +1,6 @@
-// The index arithmetic of the paged-cache kernels on the host: division by a page size, where a
-// position lies (bad pages, sequences and positions among them), and the equal runs of a list
-// of tiles.  Exits 0 when every result is the plain computation's.
+// The index arithmetic of the paged-cache entry points on the host: division by a page size,
+// where a position lies (bad pages, sequences and positions among them), rows that share
+// elements, and the equal runs of a list of tiles.  Exits 0 when every result is the plain computation's.
 #include <cstdio>
 #include <cstdlib>
 #include <random>
@@ -57,6 +57,20 @@ int main() {
         CHECK(paged_page(c, b, pos) == want);
       }
   }
+
+  // rows that share elements: as counted one by one; and strides whose products pass 64 bits
+  for (int k = 0; k < 4000; ++k) {
+    const int n = 1 + (int)(rng() % 5), T = 1 + (int)(rng() % 5), width = 1 + (int)(rng() % 6);
+    const int sub = (int)(rng() % 30), row = (int)(rng() % 30);
+    std::vector<int> used(30 * 10 + 8, 0);
+    bool want = false;
+    for (int i = 0; i < n; ++i)
+      for (int t = 0; t < T; ++t)
+        for (int c = 0; c < width; ++c) want |= used[i * sub + t * row + c]++ > 0;
+    CHECK(rows_overlap(n, T, sub, row, width) == want);
+  }
+  CHECK(!rows_overlap(65535, 1 << 22, INT64_MAX / 2, 1024, 512));
+  CHECK(rows_overlap(65535, 1 << 22, INT64_MAX / 2, INT64_MAX / 2, 512));
 
   // runs: no more than asked for, every item in the run of its quotient, and no run longer
   // than an even share rounded up

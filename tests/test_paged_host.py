@@ -85,6 +85,9 @@ def test_bad_caches_are_refused(kw, status):
     (dict(k_out=rows(row=-512)), INVALID), (dict(q_out=rows(row=128)), INVALID),
     (dict(q_out=rows(sub=0)), INVALID), (dict(k_out=rows(row=0)), INVALID),
     (dict(dtype=K.DTYPE_F32, c=cache(dtype=K.DTYPE_E4M3, scales=A)), UNSUPPORTED),
+    # strides of a row each, or that meet further on: sub-layer 1's rows are some of sub-layer 0's
+    (dict(q_out=rows(sub=256, row=256)), INVALID), (dict(q_out=rows(sub=512, row=256)), INVALID),
+    (dict(k_out=rows(sub=256, row=136)), INVALID),
 ])
 def test_append_refuses(kw, status):
     assert append(**kw) == status and K.lib().kraken_last_error()
@@ -104,6 +107,7 @@ def test_append_of_nothing_is_nothing():
     (dict(q=rows(A + 4)), INVALID), (dict(out=rows(row=128)), INVALID),
     (dict(out=rows(sub=128)), INVALID), (dict(work=A + 4), INVALID), (dict(floats=-1), INVALID),
     (dict(dtype=K.DTYPE_F32, c=cache(dtype=K.DTYPE_E4M3, scales=A)), UNSUPPORTED),
+    (dict(out=rows(sub=256, row=256)), INVALID), (dict(out=rows(sub=512, row=256)), INVALID),
 ])
 def test_attention_refuses(kw, status):
     assert attention(**kw) == status and K.lib().kraken_last_error()
