@@ -16,8 +16,8 @@
 //
 // What bounds it: many rows, the logits read once (2048 x 51200 fp32 with the likeliest token: 78
 // us, 5.4 TB/s, as without it; with 64 alternatives 84 us).  Few rows, one block's pass over
-// 50 000 logits: 12 us (8 us without alternatives), of which the vector units are busy for half.
-// A list per wave, ranked as it fills, instead of the bound: 21 and 111 us.
+// 50 000 logits: 10 us (7 us without alternatives; its CU issues vector instructions for 43%).  A list per
+// wave, ranked as it fills, instead of the bound: 21 and 111 us.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -30,6 +30,7 @@ namespace kraken {
 namespace {
 
 constexpr int MAX_SPLITS = 8;
+constexpr int JOIN_THREADS = MAX_SPLITS * KRAKEN_MAX_TOP;    // a key each
 
 struct LogprobParams {
   const void* logits;
@@ -121,11 +122,12 @@ __device__ __forceinline__ uint32_t kth_of_256(const uint32_t* v, int k) {
   return t;
 }
 
-// Block: row r, or one of the equal shares of its vectors of 16 bytes.  A step takes GV vectors of
-// every lane (16 elements), a vector of each lane after the other, so that the lanes of a short
-// row hold as many maxima as it has vectors: with rows of 1000 fp32 in 63 lanes, 64 alternatives
-// had no bound and were bisected (4096 rows: 61 us).
-template <typename S, int NW, bool TOP>
+// Block: row r, or one of the equal shares of its vectors of 16 bytes.  A step takes GV vectors (16
+// elements) of every lane.  A wave's are adjacent (2048 x 51200 fp32: 78 us; spread over the block's
+// step, 80).  SPREAD: every lane has one before any has a second, so that a row of one step has
+// as many lanes' maxima as vectors: 1000 fp32 in 63 lanes left 64 alternatives without a bound,
+// for bisection (4096 rows: 61 us, now 22).
+template <typename S, int NW, bool TOP, bool SPREAD>
 __global__ __launch_bounds__(NW * 64) void logprob_kernel(LogprobParams p) {
   constexpr int VPT = 16 / sizeof(S), GV = 16 / VPT, E = 16, THREADS = NW * 64;
   constexpr int PIECES = TOP ? 8 : 1, CAP = 512;
@@ -153,16 +155,21 @@ __global__ __launch_bounds__(NW * 64) void logprob_kernel(LogprobParams p) {
   const int per = (nv + p.splits - 1) / p.splits;
   const int v0 = share * per, v1 = min(v0 + per, nv);
   const int whole = min(nv - 1, v1);          // vectors 1 .. whole - 1 lie inside the row
+  constexpr int STEP = THREADS * GV;
+  const int steps = v1 > v0 ? (v1 - v0 + STEP - 1) / STEP : 0;
+  // from a wave's first vector of a step to the next wave's, and from a lane's vector to its next
+  constexpr int PER_WAVE = SPREAD ? 64 : 64 * GV, NEXT = SPREAD ? THREADS : 64;
+  const int mine = v0 + wave * PER_WAVE;
   auto load = [&](int first, uint4* raw) {
-    if (first > 0 && first + (GV - 1) * THREADS + 64 <= whole) {
+    if (first > 0 && first + (GV - 1) * NEXT + 64 <= whole) {
       const uint4* from = reinterpret_cast<const uint4*>(base) + first + lane;
 #pragma unroll
-      for (int g = 0; g < GV; ++g) raw[g] = from[g * THREADS];
+      for (int g = 0; g < GV; ++g) raw[g] = from[g * NEXT];
       return;
     }
 #pragma unroll
     for (int g = 0; g < GV; ++g) {
-      const int v = first + g * THREADS + lane;
+      const int v = first + g * NEXT + lane;
       if (v > 0 && v < nv - 1 && v < v1) {
         raw[g] = *reinterpret_cast<const uint4*>(base + (int64_t)v * VPT);
       } else {                                // an edge of the row, or nothing of ours
@@ -184,9 +191,6 @@ __global__ __launch_bounds__(NW * 64) void logprob_kernel(LogprobParams p) {
       for (int e = 0; e < VPT; ++e) x[g * VPT + e] = (float)c[e];
     }
   };
-  constexpr int STEP = THREADS * GV;
-  const int mine = v0 + wave * 64;            // the wave's first vectors; a step later, STEP on
-  const int steps = v1 > v0 ? (v1 - v0 + STEP - 1) / STEP : 0;
   const int piece = (steps + PIECES - 1) / PIECES;     // steps of a piece
 
   Sums a = {-INFINITY, 0.f, 0.f};
@@ -267,7 +271,7 @@ __global__ __launch_bounds__(NW * 64) void logprob_kernel(LogprobParams p) {
         unpack(again, x);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const int v = first + (e / VPT) * THREADS + lane;
+          const int v = first + (e / VPT) * NEXT + lane;
           const int64_t c = (int64_t)v * VPT + e % VPT - off;
           if (ours(v, c)) fn(order_of(x[e]), (int)c);
         }
@@ -288,7 +292,7 @@ __global__ __launch_bounds__(NW * 64) void logprob_kernel(LogprobParams p) {
       for (int i = 0; i < piece; ++i)
         for (int q = tid; q < n_pieces * GV; q += THREADS) {
           const int who = pieces[q / GV], of = who % THREADS, step = who / THREADS * piece + i;
-          const int v = v0 + step * STEP + q % GV * THREADS + of;
+          const int v = v0 + step * STEP + of / 64 * PER_WAVE + q % GV * NEXT + of % 64;
           if (step >= steps || v >= v1) continue;
           const int64_t c0 = (int64_t)v * VPT - off;
           if (v > 0 && v < nv - 1) {
@@ -373,12 +377,11 @@ __global__ __launch_bounds__(NW * 64) void logprob_kernel(LogprobParams p) {
   }
 }
 
-// Block: the shares of one row.
+// Block: the shares of one row.  Their keys are sorted, so a key's rank is the sum of what binary
+// searches find in front of it in every share.
 template <typename S>
-__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobParams p) {
-  __shared__ uint64_t keys[MAX_SPLITS * KRAKEN_MAX_TOP];
-  __shared__ unsigned long long bound;
-  __shared__ int n_keys;
+__global__ __launch_bounds__(JOIN_THREADS) void logprob_join_kernel(LogprobParams p) {
+  __shared__ uint64_t keys[JOIN_THREADS];
   const int r = blockIdx.x, tid = threadIdx.x;
   Sums a = {-INFINITY, 0.f, 0.f};
   for (int k = 0; k < p.splits; ++k) {
@@ -394,49 +397,56 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobParams p) {
         logit = (float)(static_cast<const S*>(p.logits) + r * p.ld)[token];
     }
     write_row(p, r, a, logit, token);
-    bound = 0;
-    n_keys = 0;
   }
   if (p.top == 0) return;
-  const uint64_t* in = p.keys + (int64_t)r * p.splits * p.top;
+  const int total = p.splits * p.top;
+  const uint64_t mine = tid < total ? p.keys[(int64_t)r * total + tid] : 0;    // 0: none
+  keys[tid] = mine;
   __syncthreads();
-  for (int k = tid; k < p.splits; k += 256)
-    atomicMax(&bound, (unsigned long long)in[(k + 1) * p.top - 1]);
-  __syncthreads();
-  const uint64_t b = bound;
-  for (int e = tid; e < p.splits * p.top; e += 256) {
-    const uint64_t key = in[e];
-    if (key != 0 && key >= b) keys[atomicAdd(&n_keys, 1)] = key;
+  if (mine == 0) return;
+  int before[MAX_SPLITS] = {};
+  for (int step = 1 << (31 - __builtin_clz(p.top)); step > 0; step >>= 1) {
+#pragma unroll
+    for (int k = 0; k < MAX_SPLITS; ++k) {
+      const int to = before[k] + step;          // the first `to` keys of share k
+      const uint64_t key = keys[min(k * p.top + to, JOIN_THREADS) - 1];
+      before[k] = to <= p.top && k < p.splits && key > mine ? to : before[k];
+    }
   }
-  __syncthreads();
-  const float ls = logf(a.s);
-  rank_keys<256>(keys, n_keys, p.top,
-                 [&](int rank, uint64_t key) { write_key(p, r, rank, key, a.m, ls); });
+  int rank = 0;
+#pragma unroll
+  for (int k = 0; k < MAX_SPLITS; ++k) rank += before[k];
+  if (rank < p.top) write_key(p, r, rank, mine, a.m, logf(a.s));
 }
 
-// Blocks per row.  One block of 16 waves takes 12 us for 51200 logits and 20 us for 160000 (fp32,
-// 5 alternatives); four and the join of their parts 12 and 14 us.  So long rows are shared out
-// where that leaves no block waiting for a CU.
+// Blocks per row.  A block of 8 waves takes 10 us for 51200 logits and 19 us for 160000 (fp32, the
+// likeliest token; 12 and 21 us with 64), eight and the join of their parts 11 us for 160000 (14
+// with 64), three 10.4 us for 64000 bf16 (one: 11.2).  So long rows are shared out where that
+// leaves no block waiting for a CU.
 int splits_of(int rows, int vocab) {
-  if (vocab < 80000 || rows > 128 || rows < 1) return 1;
-  return std::min({vocab / 40000, 256 / rows, MAX_SPLITS});
+  if (vocab < 60000 || rows > 128 || rows < 1) return 1;
+  return std::min({vocab / 20000, 256 / rows, MAX_SPLITS});
 }
 
-template <typename S, int NW>
+template <typename S, int NW, bool SPREAD>
 void launch_logprobs(const LogprobParams& p, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)p.rows * p.splits)), block(NW * 64);
-  if (p.top > 0) hipLaunchKernelGGL((logprob_kernel<S, NW, true>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((logprob_kernel<S, NW, false>), grid, block, 0, s, p);
+  if (p.top > 0) hipLaunchKernelGGL((logprob_kernel<S, NW, true, SPREAD>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((logprob_kernel<S, NW, false, false>), grid, block, 0, s, p);
 }
 
 template <typename S>
 hipError_t launch_typed(const LogprobParams& p, hipStream_t s) {
-  // 8 blocks of 4 waves share a CU, one of 16 has it alone: many rows stream better, few end sooner
-  if (p.rows * (int64_t)p.splits >= 512) launch_logprobs<S, 4>(p, s);
-  else launch_logprobs<S, 16>(p, s);
+  // Many rows stream better in blocks of 4 waves (1000 x 16000 fp32 with the likeliest token: 16
+  // us, of 8 waves 19), and rows that one step of such a block holds end sooner (511 x 2000: 6.4
+  // and 7.8); few long ones with 8 (1 x 51200: 10.0, with 4 11.8, with 16 11.3; 511 x 30000 bf16:
+  // 13, 15 and 19).
+  if (p.vocab <= 4096) launch_logprobs<S, 4, true>(p, s);
+  else if (p.rows * (int64_t)p.splits >= 512) launch_logprobs<S, 4, false>(p, s);
+  else launch_logprobs<S, 8, false>(p, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  hipLaunchKernelGGL(logprob_join_kernel<S>, dim3((unsigned)p.rows), dim3(256), 0, s, p);
+  hipLaunchKernelGGL(logprob_join_kernel<S>, dim3((unsigned)p.rows), dim3(JOIN_THREADS), 0, s, p);
   return hipGetLastError();
 }
 

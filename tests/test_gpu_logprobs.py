@@ -62,6 +62,7 @@ def make(rows, vocab, dtype, seed, pad=0, offset=0):
     (7, 1000, 20, 3, 1), (1, 4099, 64, 0, 0), (300, 513, 1, 0, 0), (2, 50257, 20, 0, 0),
     (1, 51200, 5, 0, 0), (3, 51200, 0, 0, 1), (1, 200003, 40, 0, 0), (61, 50257, 20, 47, 0),
     (600, 2050, 64, 0, 0), (700, 1000, 64, 0, 0), (600, 520, 64, 3, 1), (9, 1025, 64, 0, 2),
+    (5, 60007, 64, 1, 1), (128, 60000, 3, 0, 0), (2, 4096, 64, 1, 1), (513, 4097, 5, 0, 0),
 ])
 def test_rows(dtype, rows, vocab, top, pad, offset):
     print(f"[logprobs] {rows} x {vocab} top {top} pad {pad} offset {offset} {dtype}", flush=True)
