@@ -16,8 +16,8 @@
 //
 // What bounds it: many rows, the logits read once (2048 x 51200 fp32 with the likeliest token: 78
 // us, 5.4 TB/s, as without it; with 64 alternatives 84 us).  Few rows, one block's pass over
-// 50 000 logits: 10 us (7 us without alternatives; its CU issues vector instructions for 43%).  A list per
-// wave, ranked as it fills, instead of the bound: 21 and 111 us.
+// 50 000 logits: 10 us (7 us without alternatives; its CU issues vector instructions for 43% of
+// that).  A list per wave, ranked as it fills, instead of the bound: 21 and 111 us.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
